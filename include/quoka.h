@@ -253,6 +253,58 @@ quoka_status quoka_prefill_chunk_static(const quoka_params* p, const void* q, co
                                         const void* v_cache, void* out, int32_t* k_idx_out, int32_t* k_cnt_out,
                                         void* stream);
 
+/* ---- microscaled KV cache ---------------------------------------------------------------------
+ * (No counterpart in the paper: a cache of 8 or 4 bits an element under the same method.)  The calls below are those above on a
+ * cache whose rows are held in blocks of 32 elements.  A block has one scale byte b, which stands for 2^(b - 127), and
+ * 32 elements: e4m3 bytes (QUOKA_KV_MXFP8) or e2m1 nibbles (QUOKA_KV_MXFP4, two to a byte, the even element in the low one).
+ * quoka_append_kv_mx picks the smallest e with (largest magnitude of the block) <= M * 2^e, M = 448 or 6, limited to -64 <= e <= 15,
+ * writes b = e + 127 and the values times 2^-e rounded to nearest, ties to even (beyond M * 2^15 = 14680064 or 196608 they
+ * saturate).  A block with a value that is not finite gets b = 255 and elements of zero, and reads as NaN throughout.
+ * Scales outside 63 .. 142 other than 255 (a cache that other code wrote) are read by quoka_read_kv_mx and the scalar kernels
+ * (impl = QUOKA_IMPL_SIMT) only; elsewhere their values are undefined.
+ *
+ * Every value of such a cache is a bf16 number exactly: attention and scores are those of a bf16 cache that holds the values
+ * quoka_read_kv_mx returns, with the same sums (bf16 softmax weights, fp32 accumulation).
+ *
+ * quoka_params describes the cache as ever, strides in ELEMENTS (two to a byte for MXFP4), multiples of 32.  dtype is the type of
+ * q, qbar, out, of the rows appended and of those read back.  f32 queries take the scalar kernels.  The chunk's own rows
+ * are read from the cache too: append them first.  A key that is not finite makes the rows that see it NaN, a value those
+ * rows' 32 columns of its block; rows that do not see it are not touched by it.  Such a key scores minus infinity (the mean over
+ * queries: NaN). */
+typedef enum { QUOKA_KV_MXFP8 = 1, QUOKA_KV_MXFP4 = 2 } quoka_kv_format;
+typedef struct {
+  int32_t format;      /* quoka_kv_format */
+  uint8_t* k_scale;    /* DEVICE scale bytes of the keys and values, head_dim / 32 per row, indexed like the cache without head_dim:  */
+  uint8_t* v_scale;    /* contiguous [b][n_KV][kv_rows][head_dim / 32], paged [page][n_KV][64][head_dim / 32]; 16-byte aligned.
+                          Only quoka_append_kv_mx writes them. */
+} quoka_mx_cache;
+
+/* Workspace of the calls below, in the manner of quoka_workspace_size. */
+quoka_status quoka_workspace_size_mx(const quoka_params* p, const quoka_mx_cache* mx, size_t* bytes);
+
+/* quoka_append_kv into a microscaled cache: k_new, v_new dense [b][n_KV][C][d] of `dtype`.  k_inv_norm, where not NULL, gets the
+ * inverse norms of the appended rows as the cache holds them. */
+quoka_status quoka_append_kv_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* k_new, const void* v_new, void* k_cache,
+                                void* v_cache, float* k_inv_norm, void* ws, size_t ws_bytes, void* stream);
+
+/* Rows first_row .. first_row + n_rows - 1 of every (sequence, KV head) as plain tensors, dense [b][n_KV][n_rows][d] of `dtype`.
+ * first_row = QUOKA_FROM_CTX_LEN begins at T_s (read on the device).  Rows at and beyond T_s + C are left as they were in k_out
+ * and v_out.  v_cache and v_out may both be NULL. */
+#define QUOKA_FROM_CTX_LEN (-1)
+quoka_status quoka_read_kv_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* k_cache, const void* v_cache, int32_t first_row,
+                              int32_t n_rows, void* k_out, void* v_out, void* ws, size_t ws_bytes, void* stream);
+
+/* quoka_score_keys, quoka_sparse_attn, quoka_dense_chunk_attn and quoka_prefill_chunk over a microscaled cache.  With a
+ * chunk_len of 1 they are the generation step's. */
+quoka_status quoka_score_keys_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* qbar, const void* k_cache, float* scores, void* ws,
+                                 size_t ws_bytes, void* stream);
+quoka_status quoka_sparse_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
+                                  const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
+                                       void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
+                                    void* out, int32_t* k_idx_out, int32_t* k_cnt_out, void* ws, size_t ws_bytes, void* stream);
+
 /* Copies the device status word of `ws` to the host (synchronises `stream`) and
  * clears it.  *status_out is a quoka_status.  ws == NULL reads the status word of the built-in
  * array that quoka_prefill_chunk_static uses on the current device.  After a QUOKA_ERR_TIMEOUT the

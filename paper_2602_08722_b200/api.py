@@ -24,12 +24,17 @@ BF16, F32 = 0, 1
 IMPL_AUTO, IMPL_SIMT, IMPL_TENSOR = 0, 1, 2
 SCORE_COSINE, SCORE_DOT = 0, 1
 AGG_MAX, AGG_MEAN = 0, 1
+KV_NATIVE, KV_MXFP8, KV_MXFP4 = 0, 1, 2       # the cache holds `dtype`, or microscaled blocks of 8 or 4 bits an element
+MX_BLOCK = 32
+FROM_CTX_LEN = -1
 
 EXPORTS = [
     "quoka_kv_budget_cap", "quoka_workspace_size", "quoka_select_queries", "quoka_score_keys",
     "quoka_update_key_norms", "quoka_select_keys", "quoka_sparse_attn", "quoka_dense_chunk_attn", "quoka_prefill_chunk",
     "quoka_prefill_chunk_host", "quoka_prefill_chunk_static", "quoka_last_device_status", "quoka_status_string", "quoka_launch_count",
     "quoka_append_kv", "quoka_check_block_table", "quoka_selftest_wait_timeout",
+    "quoka_workspace_size_mx", "quoka_append_kv_mx", "quoka_read_kv_mx", "quoka_score_keys_mx", "quoka_sparse_attn_mx",
+    "quoka_dense_chunk_attn_mx", "quoka_prefill_chunk_mx",
 ]
 
 
@@ -53,6 +58,10 @@ class QuokaParams(C.Structure):
         ("score_mode", C.c_int32), ("query_agg", C.c_int32),
         ("k_inv_norm", C.c_void_p),
     ]
+
+
+class QuokaMxCache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p)]
 
 
 def load():
@@ -97,6 +106,14 @@ def _open(path):
     lib.quoka_append_kv.argtypes = [pp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.quoka_check_block_table.argtypes = [pp, vp, vp]
     lib.quoka_selftest_wait_timeout.argtypes = [vp, C.c_int64, vp, vp]
+    pm = C.POINTER(QuokaMxCache)
+    lib.quoka_workspace_size_mx.argtypes = [pp, pm, C.POINTER(C.c_size_t)]
+    lib.quoka_append_kv_mx.argtypes = [pp, pm, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.quoka_read_kv_mx.argtypes = [pp, pm, vp, vp, C.c_int32, C.c_int32, vp, vp, vp, sz, vp]
+    lib.quoka_score_keys_mx.argtypes = [pp, pm, vp, vp, vp, vp, sz, vp]
+    lib.quoka_sparse_attn_mx.argtypes = [pp, pm, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.quoka_dense_chunk_attn_mx.argtypes = [pp, pm, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.quoka_prefill_chunk_mx.argtypes = [pp, pm, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     for name in EXPORTS:
         if name not in ("quoka_status_string", "quoka_launch_count"):
             getattr(lib, name).restype = C.c_int
@@ -134,9 +151,10 @@ def _check(status: int, where: str):
 
 def make_params(q, k_cache, out, ctx_len, *, n_retain, kv_budget=0, budget_frac=0.0, max_ctx_len,
                 block_table=None, impl=IMPL_AUTO, softmax_scale=0.0, score_mode=SCORE_COSINE,
-                query_agg=AGG_MAX) -> QuokaParams:
+                query_agg=AGG_MAX, kv_format=KV_NATIVE) -> QuokaParams:
     """Fill quoka_params from tensors: q/out (b, n_Q, C, d); k_cache (b, n_KV, rows, d)
-    contiguous or (pages, n_KV, 64, d) with a block table (b, max_pages)."""
+    contiguous or (pages, n_KV, 64, d) with a block table (b, max_pages).  A microscaled cache
+    (kv_format) is of bytes: the last dimension is d for KV_MXFP8 and d / 2 for KV_MXFP4."""
     b, n_q, c, d = q.shape
     p = QuokaParams()
     p.batch, p.n_q_heads, p.n_kv_heads, p.head_dim = b, n_q, k_cache.shape[1], d
@@ -148,7 +166,8 @@ def make_params(q, k_cache, out, ctx_len, *, n_retain, kv_budget=0, budget_frac=
     p.ctx_len = ctx_len.data_ptr()
     p.q_stride_b, p.q_stride_h, p.q_stride_t = q.stride(0), q.stride(1), q.stride(2)
     p.o_stride_b, p.o_stride_h, p.o_stride_t = out.stride(0), out.stride(1), out.stride(2)
-    p.kv_stride_b, p.kv_stride_h, p.kv_stride_t = k_cache.stride(0), k_cache.stride(1), k_cache.stride(2)
+    per = 2 if kv_format == KV_MXFP4 else 1              # elements to a byte; strides are in elements
+    p.kv_stride_b, p.kv_stride_h, p.kv_stride_t = k_cache.stride(0) * per, k_cache.stride(1) * per, k_cache.stride(2) * per
     if block_table is None:
         p.page_size, p.max_pages_per_seq, p.block_table = 0, 0, None
         p.kv_rows = k_cache.shape[2]
@@ -156,6 +175,20 @@ def make_params(q, k_cache, out, ctx_len, *, n_retain, kv_budget=0, budget_frac=
         p.page_size, p.max_pages_per_seq, p.block_table = 64, block_table.shape[1], block_table.data_ptr()
         p.kv_rows = k_cache.shape[0]
     return p
+
+
+def make_mx_cache(kv_format, k_scale, v_scale) -> QuokaMxCache:
+    """Describe a microscaled cache: k_scale, v_scale are uint8 tensors of the cache's shape with d / 32 scale bytes
+    in the place of a row's elements, dense (contiguous (b, n_KV, rows, d / 32) or (pages, n_KV, 64, d / 32))."""
+    if not (k_scale.is_contiguous() and v_scale.is_contiguous()):
+        raise ValueError("the scale tensors of a microscaled cache are dense")
+    return QuokaMxCache(int(kv_format), k_scale.data_ptr(), v_scale.data_ptr())
+
+
+def alloc_mx_cache(rows_shape, head_dim, kv_format, device="cuda"):
+    """A zeroed microscaled cache, (k, v, k_scale, v_scale) of uint8: rows_shape is (b, n_KV, rows), or (pages, n_KV, 64)."""
+    row = head_dim if kv_format == KV_MXFP8 else head_dim // 2
+    return tuple(torch.zeros(*rows_shape, n, dtype=torch.uint8, device=device) for n in (row, row, head_dim // MX_BLOCK, head_dim // MX_BLOCK))
 
 
 def quoka_kv_budget_cap(p: QuokaParams) -> int:
@@ -170,9 +203,11 @@ def quoka_workspace_size(p: QuokaParams) -> int:
     return n.value
 
 
-def alloc_workspace(p: QuokaParams, device="cuda") -> torch.Tensor:
-    """A zeroed uint8 tensor of quoka_workspace_size bytes (torch's allocator is 512-byte aligned)."""
-    return torch.zeros(quoka_workspace_size(p), dtype=torch.uint8, device=device)
+def alloc_workspace(p: QuokaParams, device="cuda", mx=None) -> torch.Tensor:
+    """A zeroed uint8 tensor of quoka_workspace_size bytes (torch's allocator is 512-byte aligned), with `mx` of
+    quoka_workspace_size_mx bytes."""
+    n = quoka_workspace_size(p) if mx is None else quoka_workspace_size_mx(p, mx)
+    return torch.zeros(n, dtype=torch.uint8, device=device)
 
 
 def quoka_select_queries(p, q, q_idx, qbar, ws, stream=None):
@@ -237,6 +272,42 @@ def quoka_last_device_status(ws, stream=None) -> int:
 def quoka_append_kv(p, k_new, v_new, k_cache, v_cache, k_inv_norm, ws, stream=None):
     _check(load().quoka_append_kv(C.byref(p), _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache),
                                   _ptr(k_inv_norm), _ptr(ws), ws.numel(), _stream(stream)), "quoka_append_kv")
+
+
+def quoka_workspace_size_mx(p: QuokaParams, mx: QuokaMxCache) -> int:
+    n = C.c_size_t(0)
+    _check(load().quoka_workspace_size_mx(C.byref(p), C.byref(mx), C.byref(n)), "quoka_workspace_size_mx")
+    return n.value
+
+
+def quoka_append_kv_mx(p, mx, k_new, v_new, k_cache, v_cache, k_inv_norm, ws, stream=None):
+    _check(load().quoka_append_kv_mx(C.byref(p), C.byref(mx), _ptr(k_new), _ptr(v_new), _ptr(k_cache), _ptr(v_cache), _ptr(k_inv_norm),
+                                     _ptr(ws), ws.numel(), _stream(stream)), "quoka_append_kv_mx")
+
+
+def quoka_read_kv_mx(p, mx, k_cache, v_cache, first_row, n_rows, k_out, v_out, ws, stream=None):
+    _check(load().quoka_read_kv_mx(C.byref(p), C.byref(mx), _ptr(k_cache), _ptr(v_cache), int(first_row), int(n_rows), _ptr(k_out),
+                                   _ptr(v_out), _ptr(ws), ws.numel(), _stream(stream)), "quoka_read_kv_mx")
+
+
+def quoka_score_keys_mx(p, mx, qbar, k_cache, scores, ws, stream=None):
+    _check(load().quoka_score_keys_mx(C.byref(p), C.byref(mx), _ptr(qbar), _ptr(k_cache), _ptr(scores), _ptr(ws), ws.numel(),
+                                      _stream(stream)), "quoka_score_keys_mx")
+
+
+def quoka_sparse_attn_mx(p, mx, q, k_cache, v_cache, k_idx, k_cnt, out, lse, ws, stream=None):
+    _check(load().quoka_sparse_attn_mx(C.byref(p), C.byref(mx), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_idx), _ptr(k_cnt),
+                                       _ptr(out), _ptr(lse), _ptr(ws), ws.numel(), _stream(stream)), "quoka_sparse_attn_mx")
+
+
+def quoka_dense_chunk_attn_mx(p, mx, q, k_cache, v_cache, out, lse, ws, stream=None):
+    _check(load().quoka_dense_chunk_attn_mx(C.byref(p), C.byref(mx), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(lse),
+                                            _ptr(ws), ws.numel(), _stream(stream)), "quoka_dense_chunk_attn_mx")
+
+
+def quoka_prefill_chunk_mx(p, mx, q, k_cache, v_cache, out, k_idx_out, k_cnt_out, ws, stream=None):
+    _check(load().quoka_prefill_chunk_mx(C.byref(p), C.byref(mx), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(out), _ptr(k_idx_out),
+                                         _ptr(k_cnt_out), _ptr(ws), ws.numel(), _stream(stream)), "quoka_prefill_chunk_mx")
 
 
 def quoka_check_block_table(p, ctx_len_host, block_table_host) -> int:

@@ -34,6 +34,8 @@ struct DevParams {
   int agg_mean;     // 1: mean over the retained queries instead of the maximum
   const float* k_inv_norm;  // cached 1/|k| per cache row, or null
   int64_t kv_rows;  // rows per (sequence, head) when contiguous
+  const uint8_t* k_scale;   // scale bytes of a microscaled cache (mx.cuh), else null
+  const uint8_t* v_scale;
   // split attention (small grids): room for the parts' partial results and their arrival counters, or null
   float* attn_partials;
   int32_t* attn_counters;

@@ -1,0 +1,64 @@
+// The microscaled cache format on the device.
+//
+// A row of D elements is D / 32 blocks.  A block is one scale byte b, standing for 2^(b - 127), and 32 elements: e4m3 bytes
+// (MXFP8), or e2m1 nibbles (MXFP4), two to a byte, the even element in the low one.  A scale is a power of two and an element
+// has at most four significant bits, so every value of the cache is a bf16 number exactly: products of queries with it are
+// those of a bf16 cache that holds the same values, and nothing is rounded when it is read.
+#pragma once
+
+#include "common.cuh"
+
+namespace quoka {
+
+constexpr int kMxBlock = 32;
+constexpr int kMxExpMin = -64, kMxExpMax = 15;    // exponents of a scale, as quoka_append_kv_mx writes them
+constexpr uint32_t kMxNanScale = 255;             // a block with a value that is not finite reads back as NaN
+
+template <int FMT>
+constexpr int kMxBits = FMT == QUOKA_KV_MXFP8 ? 8 : 4;
+
+// The value of an element: its bits at the place of an fp32 number's exponent and fraction are the value times a power of two
+// (subnormals too), which the multiplication takes off.
+template <int FMT>
+__device__ __forceinline__ float mx_element(uint32_t code) {
+  if constexpr (FMT == QUOKA_KV_MXFP8)
+    return __uint_as_float((code & 0x80u) << 24 | (code & 0x7Fu) << 20) * 0x1p120f;
+  else
+    return __uint_as_float((code & 8u) << 28 | (code & 7u) << 22) * 0x1p126f;
+}
+
+// 2^(b - 127), NaN for the scale byte of a block that is not finite.
+__device__ __forceinline__ float mx_scale(uint32_t b) {
+  return b == kMxNanScale ? __uint_as_float(0x7FC00000u) : b == 0 ? 0x1p-127f : __uint_as_float(b << 23);
+}
+
+// Exponent of a block's scale from the bits of its largest magnitude (finite): the smallest e with amax <= M 2^e, M = 1.75 2^8 or
+// 1.5 2^2: a fraction above M's carries into the exponent.
+template <int FMT>
+__device__ __forceinline__ int mx_scale_exponent(uint32_t amax_bits) {
+  constexpr uint32_t kCarry = FMT == QUOKA_KV_MXFP8 ? 0x1FFFFFu : 0x3FFFFFu;
+  const int e = (int)((amax_bits + kCarry) >> 23) - 127 - (FMT == QUOKA_KV_MXFP8 ? 8 : 2);
+  return min(max(e, kMxExpMin), kMxExpMax);
+}
+
+// Two values, already divided by their scale, to elements (round to nearest even, saturating): a in the lower one.
+template <int FMT>
+__device__ __forceinline__ uint32_t mx_encode2(float a, float b) {
+  if constexpr (FMT == QUOKA_KV_MXFP8) {
+    uint16_t h;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(h) : "f"(b), "f"(a));
+    return h;
+  } else {
+    uint32_t w;
+    asm("{\n\t.reg .b8 t;\n\tcvt.rn.satfinite.e2m1x2.f32 t, %1, %2;\n\tmov.b32 %0, {t, t, t, t};\n\t}" : "=r"(w) : "f"(b), "f"(a));
+    return w & 0xFFu;
+  }
+}
+
+// Index of a row's first scale byte: the cache's layout without head_dim, D / 32 bytes per row.
+template <int D, bool FIRST = false>
+__device__ __forceinline__ int64_t mx_scale_index(const DevParams& P, int s, int h, int t) {
+  return kv_norm_index<FIRST>(P, s, h, t) * (D / kMxBlock);
+}
+
+}  // namespace quoka

@@ -8,8 +8,7 @@
 
 #include <mutex>
 
-#include "common.cuh"
-#include "tensor_kernels.cuh"
+#include "api_host.cuh"
 
 namespace quoka {
 
@@ -18,27 +17,14 @@ void count_launch(int n) { g_launches.fetch_add(n, std::memory_order_relaxed); }
 
 static inline size_t align_up(size_t x, size_t a = 256) { return (x + a - 1) / a * a; }
 
-struct Workspace {
-  int32_t* status;
-  int32_t* q_idx;
-  void* qbar;
-  float* scores;
-  int32_t* k_idx;
-  int32_t* k_cnt;
-  float* attn_partials;      // split attention of small grids: partial results and arrival counters, or null
-  int32_t* attn_counters;
-  int n_attn_counters;
-  size_t total;
-};
-
-static int budget_cap_of(const quoka_params* p) {
+int budget_cap_of(const quoka_params* p) {
   int cap = key_budget(p->max_ctx_len, p->kv_budget, p->budget_frac);
   return cap < 1 ? 1 : cap;
 }
 
 // The buffers of a call in a workspace of ws_bytes.  The scratch of `plan` (partial results and arrival counters of row
 // blocks in parts that merge through memory), where the plan has any, comes last.
-static Workspace carve(const quoka_params* p, void* ws, size_t ws_bytes = 0, const AttnPlan* plan = nullptr) {
+Workspace carve(const quoka_params* p, void* ws, size_t ws_bytes, const AttnPlan* plan) {
   Workspace w{};
   const size_t es = p->dtype == QUOKA_BF16 ? 2 : 4;
   const int N = p->n_retain < p->chunk_len ? p->n_retain : p->chunk_len;
@@ -67,7 +53,7 @@ static Workspace carve(const quoka_params* p, void* ws, size_t ws_bytes = 0, con
 }
 
 // What a workspace of ws_bytes has left for the scratch of a plan.
-static size_t attn_room(const quoka_params* p, size_t ws_bytes) {
+size_t attn_room(const quoka_params* p, size_t ws_bytes) {
   const size_t least = carve(p, nullptr).total;
   return ws_bytes > least ? ws_bytes - least : 0;
 }
@@ -94,7 +80,7 @@ static size_t attn_scratch_of_shorter_chunks(const quoka_params* p) {
   return bytes;
 }
 
-static quoka_status validate(const quoka_params* p) {
+quoka_status validate(const quoka_params* p) {
   if (!p) return QUOKA_ERR_INVALID_ARG;
   if (p->batch <= 0 || p->n_q_heads <= 0 || p->n_kv_heads <= 0 || p->chunk_len <= 0 || p->n_retain <= 0)
     return QUOKA_ERR_INVALID_ARG;
@@ -122,7 +108,7 @@ static quoka_status validate(const quoka_params* p) {
   return QUOKA_OK;
 }
 
-static bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) == 0; }
+bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) == 0; }
 
 // Everything the fused call checks before it touches the stream, except the workspace.
 quoka_status check_prefill_args(const quoka_params* p, const void* q, const void* k_cache, const void* v_cache,
@@ -136,7 +122,7 @@ quoka_status check_prefill_args(const quoka_params* p, const void* q, const void
   return QUOKA_OK;
 }
 
-static quoka_status check_ws(const quoka_params* p, void* ws, size_t ws_bytes) {
+quoka_status check_ws(const quoka_params* p, void* ws, size_t ws_bytes) {
   if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255) != 0) return QUOKA_ERR_WORKSPACE;
   if (ws_bytes < carve(p, nullptr).total) return QUOKA_ERR_WORKSPACE;       // the attention's scratch may be missing
   return QUOKA_OK;
@@ -144,7 +130,7 @@ static quoka_status check_ws(const quoka_params* p, void* ws, size_t ws_bytes) {
 
 size_t workspace_bytes_unsplit(const quoka_params* p) { return carve(p, nullptr).total; }
 
-static DevParams make_dev(const quoka_params* p, void* ws, const Workspace& w) {
+DevParams make_dev(const quoka_params* p, void* ws, const Workspace& w) {
   DevParams P{};
   P.batch = p->batch; P.n_q = p->n_q_heads; P.n_kv = p->n_kv_heads; P.group = p->n_q_heads / p->n_kv_heads;
   P.d = p->head_dim; P.chunk = p->chunk_len; P.n_retain = p->n_retain;
@@ -168,7 +154,7 @@ static DevParams make_dev(const quoka_params* p, void* ws, const Workspace& w) {
   P.attn_pack = 1; P.attn_span = 128; P.attn_qtiles = 2;
   return P;
 }
-static DevParams make_dev(const quoka_params* p, void* ws) { return make_dev(p, ws, carve(p, ws)); }
+DevParams make_dev(const quoka_params* p, void* ws) { return make_dev(p, ws, carve(p, ws)); }
 
 static bool use_tensor(const quoka_params* p) {
   if (p->impl == QUOKA_IMPL_SIMT) return false;
@@ -176,15 +162,9 @@ static bool use_tensor(const quoka_params* p) {
   return true;
 }
 
-#define QUOKA_TRY_CUDA(expr)                          \
-  do {                                                \
-    cudaError_t e_ = (expr);                          \
-    if (e_ != cudaSuccess) return QUOKA_ERR_CUDA;     \
-  } while (0)
-
 // early: launched before what is before it on the stream has completed (the first kernel waits for that itself)
-static quoka_status run_select_queries(const quoka_params* p, const DevParams& P, const void* q, int32_t* q_idx,
-                                       void* qbar, cudaStream_t st, bool early = false) {
+quoka_status run_select_queries(const quoka_params* p, const DevParams& P, const void* q, int32_t* q_idx,
+                                       void* qbar, cudaStream_t st, bool early) {
   QUOKA_TRY_CUDA(launch_rank_queries(P, p->dtype, q, q_idx, st, early));
   QUOKA_TRY_CUDA(launch_aggregate_queries(P, p->dtype, q, q_idx, qbar, st, early || P.chunk > P.n_retain));
   return QUOKA_OK;
