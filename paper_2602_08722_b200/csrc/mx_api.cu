@@ -33,7 +33,10 @@ static quoka_status run_score_keys_mx(const quoka_params* p, const quoka_mx_cach
 }
 
 static quoka_status run_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const DevParams& P, const void* q, const void* k, const void* v,
-                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st) {
+                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, const AttnPlan& plan,
+                                bool after_selection = false) {
+  if (p->impl != QUOKA_IMPL_SIMT && attn_mx_tc_supported(p))
+    return launch_attn_mx_tc(p, P, mx->format, q, k, v, k_idx, k_cnt, out, lse, st, after_selection, plan);
   if (p->impl == QUOKA_IMPL_TENSOR) return QUOKA_ERR_UNSUPPORTED;
   QUOKA_TRY_CUDA(launch_attn_mx_simt(P, p->dtype, mx->format, q, k, v, k_idx, k_cnt, out, lse, st));
   return QUOKA_OK;
@@ -97,7 +100,9 @@ quoka_status quoka_sparse_attn_mx(const quoka_params* p, const quoka_mx_cache* m
   if (!q || !k_cache || !v_cache || !k_idx || !k_cnt || !out) return QUOKA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws)), q, k_cache, v_cache, k_idx, k_cnt, out, lse, static_cast<cudaStream_t>(stream));
+  const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws, ws_bytes, &plan)), q, k_cache, v_cache, k_idx, k_cnt, out, lse,
+                     static_cast<cudaStream_t>(stream), plan);
 }
 
 quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
@@ -107,7 +112,9 @@ quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cac
   if (!q || !k_cache || !v_cache || !out) return QUOKA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws)), q, k_cache, v_cache, nullptr, nullptr, out, lse, static_cast<cudaStream_t>(stream));
+  const AttnPlan plan = attn_plan_dense(p, attn_room(p, ws_bytes));
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws, ws_bytes, &plan)), q, k_cache, v_cache, nullptr, nullptr, out, lse,
+                     static_cast<cudaStream_t>(stream), plan);
 }
 
 quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
@@ -118,7 +125,8 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const Workspace w = carve(p, ws);
+  const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
+  const Workspace w = carve(p, ws, ws_bytes, &plan);
   const DevParams P = make_dev_mx(p, mx, ws, w);
   int32_t* k_idx = k_idx_out ? k_idx_out : w.k_idx;
   int32_t* k_cnt = k_cnt_out ? k_cnt_out : w.k_cnt;
@@ -127,7 +135,7 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
     if ((st = run_score_keys_mx(p, mx, P, w.qbar, k_cache, w.scores, cs)) != QUOKA_OK) return st;
   }
   QUOKA_TRY_CUDA(launch_select_keys(P, w.scores, k_idx, k_cnt, cs));
-  return run_attn_mx(p, mx, P, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs);
+  return run_attn_mx(p, mx, P, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs, plan);
 }
 
 }  // extern "C"

@@ -32,9 +32,17 @@ int attn_same_plan_up_to(const quoka_params* p, int chunk);
 quoka_status launch_attn_tc(const quoka_params* p, const DevParams& P, const void* q, const void* k, const void* v,
                             const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st,
                             bool after_selection, const AttnPlan& plan);
+// the call's parameters with the plan's row blocks
+DevParams attn_of_plan(const DevParams& P, const AttnPlan& plan);
 // plan.ctas = 2: two CTAs with neighbouring positions of a KV group work as a pair (cta_group::2, head_dim 128)
 quoka_status launch_attn_tc_pair(const quoka_params* p, const DevParams& P, const void* q, const void* k, const void* v,
                                  const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st,
                                  bool after_selection, const AttnPlan& plan);
+
+// The same over a microscaled cache (the scale arrays in P).
+bool attn_mx_tc_supported(const quoka_params* p);
+quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* q, const void* k, const void* v,
+                               const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, bool after_selection,
+                               const AttnPlan& plan);
 
 }  // namespace quoka
