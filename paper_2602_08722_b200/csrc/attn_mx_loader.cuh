@@ -11,7 +11,7 @@
 // column set it to minus infinity.  A value's block becomes zeros, as its products with weights of zero would reach rows that do not see
 // it; the first chunk position that sees one is kept per block of columns, and the epilogue makes NaN of what is at or behind it.
 //
-// What bounds it: instructions.  Five a pair of elements, 16 elements a lane and copy; loads run one copy group (8 of 16 elements a
+// What bounds it: instructions.  Five a pair of elements, 16 elements a lane and copy; loads run one copy group (4 of 16 elements a
 // lane) ahead of the conversion.
 #pragma once
 
@@ -19,6 +19,12 @@
 #include "mx.cuh"
 
 namespace quoka {
+
+// 512 threads: the roles of the bf16 kernels in the first 12 warps but for the loaders, which are the last four, one on each
+// sub-partition's issue port.  A thread may then have 128 registers; the softmax warps take 168 and the others give them.
+constexpr int kMxAttnThreads = 512, kMxLoaderWarps = 4, kMxFirstLoader = 12;
+constexpr int kMxSoftmaxRegs = 168, kMxOtherRegs = 88;
+static_assert(256 * kMxSoftmaxRegs + 256 * kMxOtherRegs == kMxAttnThreads * 128, "what the block is launched with");
 
 constexpr int kMxShift = 16;                         // tiles hold values times 2^-kMxShift
 constexpr float kMxUnshift = 65536.f;
@@ -69,9 +75,9 @@ struct MxLoader {
   static constexpr int KU = D / 16, VU = VC / 16;                      // units per row
   static constexpr int K_RPI = 32 / KU, V_RPI = 32 / VU;               // rows per warp instruction
   static constexpr int K_GROUPS = ROWS_K / (K_RPI * NLW), V_GROUPS = 128 / (V_RPI * NLW);     // row groups of this warp
-  static constexpr int SUB = K_GROUPS < 8 ? K_GROUPS : 8;              // of them at a time
+  static constexpr int SUB = 4;                                        // of them at a time
   static constexpr int KSUB = K_GROUPS / SUB, VSUB = V_GROUPS / SUB;
-  static constexpr int K_REGS = (K_GROUPS * K_RPI + 31) / 32, V_REGS = (V_GROUPS * V_RPI + 31) / 32;
+  static constexpr int K_REGS = (K_GROUPS * K_RPI + 31) / 32, V_REGS = (V_GROUPS * V_RPI + 31) / 32;     // (a lane may be left over)
   static_assert(K_GROUPS % SUB == 0 && V_GROUPS % SUB == 0 && (KSUB + VSUB) % 2 == 0, "whole groups, alternating buffers");
   // a row's number, its offset in units of 16 elements (kNoRow: no such row) and its scale bytes; lane l looks after rows p = l, 32 + l
   // of this warp's rows, p = group * rows per instruction + row of the instruction
@@ -108,13 +114,13 @@ struct MxLoader {
   template <bool V, int R> __device__ __forceinline__ void numbers(const TileRows& tr, int (&t)[R]) const {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      const int rr = tile_row<V>(r);
+      const int rr = 32 * r + lane < (V ? V_GROUPS * V_RPI : K_GROUPS * K_RPI) ? tile_row<V>(r) : 128;
       if (SPARSE && tr.from_list) {
         const int last = min(tr.count, kKeyTile) - 1;
         const int n = last >= 0 ? __ldcg(idx + tr.first + min(rr, last)) : -1;     // written by the kernel before: L2
         t[r] = rr <= last ? n : -1;
       } else {
-        t[r] = rr < tr.count ? tr.first + rr : -1;
+        t[r] = rr < min(tr.count, kKeyTile) ? tr.first + rr : -1;
       }
     }
   }

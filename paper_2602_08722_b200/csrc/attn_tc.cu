@@ -196,7 +196,7 @@ size_t attn_plan_scratch_bytes(const quoka_params* p, const AttnPlan& plan) {
 // list length (sparse: the selection is complete by then, so the parts need not wait for it), and the parts' last CTA
 // waits for the whole row blocks before it ends.
 quoka_status launch_attn_plan(const quoka_params* p, const DevParams& P, const AttnPlan& plan, AttnKernel (*pick)(bool, bool, bool),
-                              const char* name, int cluster, size_t smem, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                              const char* name, int cluster, int threads, size_t smem, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                               const CUtensorMap& tm_v, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt,
                               void* out, float* lse, cudaStream_t st, bool after_selection) {
   const bool sparse = k_idx != nullptr, split = plan.split_rb > 0 && (P.attn_partials || plan.in_cluster);
@@ -216,7 +216,7 @@ quoka_status launch_attn_plan(const quoka_params* p, const DevParams& P, const A
     const bool early = parts && whole > 0 ? true : sparse && after_selection;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(shape.per_rb / P.batch), parts ? PP.attn_split_rb * PP.attn_parts : whole, P.batch);
-    cfg.blockDim = dim3(kAttnThreads);
+    cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -285,7 +285,7 @@ quoka_status launch_attn_tc(const quoka_params* p, const DevParams& P0, const vo
   if (!encode_q_tensor_map(&tm_q, P, q)) return QUOKA_ERR_CUDA;
   if (!encode_kv_tensor_map(&tm_k, p, k, 64) || !encode_kv_tensor_map(&tm_v, p, v, 64)) return QUOKA_ERR_CUDA;
   const bool wide = P.d == 128;
-  return launch_attn_plan(p, P, plan, wide ? pick_attn_tc<128, 0> : pick_attn_tc<64, 0>, "attn_tc", /*cluster=*/1,
+  return launch_attn_plan(p, P, plan, wide ? pick_attn_tc<128, 0> : pick_attn_tc<64, 0>, "attn_tc", /*cluster=*/1, kAttnThreads,
                           wide ? kAttnSmem<128> : kAttnSmem<64>, tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse, st, after_selection);
 }
 

@@ -35,13 +35,14 @@ template <int D>
 constexpr size_t kAttnSmem = 1024 + (size_t)(2 + kSlotsOf<D>) * (D / 64) * 16384 + 512;
 
 template <int D, bool SPARSE, bool SPLIT, int FMT = 0>
-__global__ void __launch_bounds__(kAttnThreads, 1)
+__global__ void __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1)
 attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const __nv_bfloat16* __restrict__ kc,
                const __nv_bfloat16* __restrict__ vc, const int32_t* __restrict__ k_idx,
                const int32_t* __restrict__ k_cnt, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
   constexpr int kSlots = kSlotsOf<D>, HALVES = D / 64;
   constexpr bool MX = FMT != 0;                              // a microscaled cache: kc, vc are its bytes
+  constexpr int kThreads = MX ? kMxAttnThreads : kAttnThreads;
   constexpr uint32_t kHalfBytes = 128 * 128;                 // 128 rows x 128 B
   constexpr uint32_t kTileBytes = HALVES * kHalfBytes;       // one Q / K / V tile
   // tensor memory (see "order of the products"): S | S | S | O_A | O_B, head_dim 128: S | S | O_A | O_B; P in place
@@ -87,7 +88,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int i = 0; i < kSlots; ++i) { mbar_init(&kv_full[i], MX ? kLoaderWarps : kLoaderWarps * 32); mbar_init(&kv_empty[i], 1); }
+    for (int i = 0; i < kSlots; ++i) { mbar_init(&kv_full[i], MX ? kMxLoaderWarps : kLoaderWarps * 32); mbar_init(&kv_empty[i], 1); }
     for (int i = 0; i < NBUF; ++i) { mbar_init(&s_full[i], 1); mbar_init(&p_done[i], 1); }
     for (int i = 0; i < 2 * NBUF; ++i) mbar_init(&p_full[i], 4);
     for (int i = 0; i < 2; ++i) mbar_init(&o_full[i], 1);
@@ -102,13 +103,16 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     }
   }
   if (warp == kQkWarp) tmem_alloc(tmem_slot, 512);
-  zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kAttnThreads);
+  zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
   tc_fence_before();
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem_base = *tmem_slot;
   if (!SPARSE && !SPLIT) grid_launch_dependents();
 
+  if constexpr (MX) {
+    if (warp < 8) setmaxnreg_inc<kMxSoftmaxRegs>(); else setmaxnreg_dec<kMxOtherRegs>();
+  }
   if (warp < 8) {
     // ================================================================== softmax + epilogue
     const int x = warp >> 2;                                  // Q tile A (0) or B (1)
@@ -164,12 +168,12 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
                              row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s, qr.head(P, row_in_tile),
                              out, lse, v_nan);
     }
-  } else if (warp < 8 + kLoaderWarps) {
+  } else if (MX ? warp >= kMxFirstLoader : warp < 8 + kLoaderWarps) {
     // ================================================================== K / V row loaders (gather)
     // One warp instruction copies four whole rows (eight lanes x 16 bytes cover a 128-byte row; head_dim 128: two); the row
     // groups of a tile are dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxLoader<FMT, D, 128, D, SPARSE, kLoaderWarps, kSlots> loader(P, s, kv, warp - 8, lane, 0, 0, g.T, kc, vc, k_idx, v_nan);
+      MxLoader<FMT, D, 128, D, SPARSE, kMxLoaderWarps, kSlots> loader(P, s, kv, warp - kMxFirstLoader, lane, 0, 0, g.T, kc, vc, k_idx, v_nan);
       loader.run(g, t_lo, kv_smem, kTileBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;
@@ -292,7 +296,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     cp_async_wait_all();                                      // nothing of this thread is in flight at exit
     }
-  } else {
+  } else if (!MX || warp >= kPvWarp) {
     // ================================================================== warp 11: QK^T, warp 10: PV
     if (warp == kQkWarp && lane == 0) load_q_tiles<D>(P, qr, q_smem, &tm_q, q_full, s);
     __syncwarp();
@@ -358,6 +362,12 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
           },
           release, [&](int x) { if (leader) mma_commit(&o_full[x]); });
     }
+  }
+  if constexpr (MX) {
+    // As launched, once every warp has had its share: a warp that took registers back before would keep a softmax warp from
+    // ever getting its own.
+    __syncthreads();
+    if (warp < 8) setmaxnreg_dec<128>(); else setmaxnreg_inc<128>();
   }
   if (SPLIT && attn_last_cta()) grid_dependency_wait();       // this grid's end is the whole row blocks' end too
   tc_fence_before();

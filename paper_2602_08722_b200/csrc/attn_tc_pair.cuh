@@ -47,6 +47,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
   constexpr bool SPLIT = MODE != kWhole;
   constexpr int D = 128;
   constexpr bool MX = FMT != 0;                               // a microscaled cache: kc, vc are its bytes
+  constexpr int kThreads = MX ? kMxAttnThreads : kAttnThreads;
   constexpr uint32_t S_COL = 0, P_COL = 128, O_COL = 256;     // Q tile B's P and O are 64 and 128 columns on
   extern __shared__ unsigned char smem_raw[];
   unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -85,7 +86,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
   if (threadIdx.x == 0) {
     abort_flag = 0;
     for (int i = 0; i < kPairSlots; ++i) {
-      mbar_init(&kv_full[i], MX ? kPairLoaderWarps : kPairLoaderWarps * 32);
+      mbar_init(&kv_full[i], MX ? kMxLoaderWarps : kPairLoaderWarps * 32);
       mbar_init(&kv_empty[i], 1);
       mbar_init(&peer_full[i], 1);
     }
@@ -104,7 +105,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     }
   }
   if (warp == kQkWarp) tmem_alloc_pair(tmem_slot, 512);
-  zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kAttnThreads);
+  zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
   tc_fence_before();
   cluster_sync_all();                                         // both CTAs' barriers exist before anyone signals them
   tc_fence_after();
@@ -125,6 +126,9 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
 
   if (!SPARSE && !SPLIT) grid_launch_dependents();
 
+  if constexpr (MX) {
+    if (warp < 8) setmaxnreg_inc<kMxSoftmaxRegs>(); else setmaxnreg_dec<kMxOtherRegs>();
+  }
   if (warp < 8) {
     // ================================================================== softmax + epilogue
     const int x = warp >> 2;                                  // Q tile A (0) or B (1)
@@ -183,13 +187,13 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
                              quarter, lane, row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s,
                              qr.head(P, row_in_tile), out, lse, v_nan);
     }
-  } else if (warp < 8 + kPairLoaderWarps) {
+  } else if (MX ? warp >= kMxFirstLoader : warp < 8 + kPairLoaderWarps) {
     // ================================================================== K / V loaders: this CTA's half of every tile
     // K item: tile rows [64 * rank, 64 * rank + 64), 256 bytes each (16 pieces, 2 rows per warp instruction).
     // V item: all 128 tile rows, bytes [128 * rank, 128 * rank + 128) of each (8 pieces, 4 rows per instruction).
     // Either way an item is 32 row groups, dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxLoader<FMT, D, 64, 64, SPARSE, kPairLoaderWarps, kPairSlots> loader(P, s, kv, warp - 8, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan);
+      MxLoader<FMT, D, 64, 64, SPARSE, kMxLoaderWarps, kPairSlots> loader(P, s, kv, warp - kMxFirstLoader, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan);
       loader.run(g, t_lo, kv_smem, kPairSlotBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;
@@ -300,6 +304,8 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     }
     cp_async_wait_all();                                      // nothing of this thread is in flight at exit
     }
+  } else if (MX && warp < kPvWarp) {
+    // (no role)
   } else if (rank != 0) {
     // ================================================================== second CTA, one thread of warps 10 and 11: forward
     // the "full" of the V (10) and K (11) slots to the first CTA
@@ -389,11 +395,17 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
           release, [&](int x) { if (leader) mma_pair_commit(both, &o_full[x]); });
     }
   }
+  if constexpr (MX) {
+    // As launched, once every warp has had its share: a warp that took registers back before would keep a softmax warp from
+    // ever getting its own.
+    __syncthreads();
+    if (warp < 8) setmaxnreg_dec<128>(); else setmaxnreg_inc<128>();
+  }
   if (SPLIT && attn_last_cta()) grid_dependency_wait();       // this grid's end is the whole row blocks' end too
   tc_fence_before();
   if constexpr (MODE == kPartsCluster) {
     cluster_sync_all();                                       // every part's result is in its shared memory
-    attn_merge_cluster<D, MX>(P, smem, part_ml, warp, kAttnThreads / 32, lane, 2, (int)rank, n_parts, blockIdx.y % n_parts, qr, s, out, lse);
+    attn_merge_cluster<D, MX>(P, smem, part_ml, warp, kThreads / 32, lane, 2, (int)rank, n_parts, blockIdx.y % n_parts, qr, s, out, lse);
   }
   cluster_sync_all();                                         // the other CTA's MMAs no longer read this CTA
   if (warp == kQkWarp) tmem_dealloc_pair(tmem_base, 512);
@@ -404,12 +416,12 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
       const __grid_constant__ CUtensorMap tm_v, const __nv_bfloat16 *__restrict__ kc, const __nv_bfloat16 *__restrict__ vc, \
       const int32_t *__restrict__ k_idx, const int32_t *__restrict__ k_cnt, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse
 template <bool SPARSE, bool SPLIT, int FMT = 0>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kAttnThreads, 1) attn_tc_pair_kernel(QUOKA_PAIR_PARAMS) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_kernel(QUOKA_PAIR_PARAMS) {
   attn_tc_pair_body<SPARSE, SPLIT ? kParts : kWhole, FMT>(P, tm_q, tm_k, tm_v, kc, vc, k_idx, k_cnt, out, lse);
 }
 // clusters of (2, parts): the pairs of a row block's parts
 template <bool SPARSE, int FMT = 0>
-__global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_pair_cluster_kernel(QUOKA_PAIR_PARAMS) {
+__global__ void __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_cluster_kernel(QUOKA_PAIR_PARAMS) {
   attn_tc_pair_body<SPARSE, kPartsCluster, FMT>(P, tm_q, tm_k, tm_v, kc, vc, k_idx, k_cnt, out, lse);
 }
 

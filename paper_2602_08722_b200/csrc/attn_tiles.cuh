@@ -25,7 +25,7 @@ constexpr float kRescaleThreshold = 32.0f;   // log2 units
 typedef void (*AttnKernel)(DevParams, const CUtensorMap, const CUtensorMap, const CUtensorMap, const __nv_bfloat16*,
                            const __nv_bfloat16*, const int32_t*, const int32_t*, __nv_bfloat16*, float*);
 quoka_status launch_attn_plan(const quoka_params* p, const DevParams& P, const AttnPlan& plan, AttnKernel (*pick)(bool, bool, bool),
-                              const char* name, int cluster, size_t smem, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
+                              const char* name, int cluster, int threads, size_t smem, const CUtensorMap& tm_q, const CUtensorMap& tm_k,
                               const CUtensorMap& tm_v, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt,
                               void* out, float* lse, cudaStream_t st, bool after_selection);
 
