@@ -11,9 +11,11 @@
 // column set it to minus infinity.  A value's block becomes zeros, as its products with weights of zero would reach rows that do not see
 // it; the first chunk position that sees one is kept per block of columns, and the epilogue makes NaN of what is at or behind it.
 //
-// What bounds it: instructions.  Five a pair of elements, 16 elements a lane and copy; loads run one copy group (4 of 16 elements a
-// lane) ahead of the conversion.
+// What bounds it: instructions.  Five a pair of elements, 16 elements a lane and copy; copies run two or three
+// items ahead of the conversion.
 #pragma once
+
+#include <type_traits>
 
 #include "attn_tiles.cuh"
 #include "mx.cuh"
@@ -70,29 +72,33 @@ __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t
 
 // One loader warp of NLW.  A K item of the ring is ROWS_K tile rows from row k_row0 on, all D columns; a V item all 128 rows, VC columns
 // from v_col0 on.  Both are [64-column halves][rows][128 B], 16-byte pieces swizzled by row.
-template <int FMT, int D, int ROWS_K, int VC, bool SPARSE, int NLW, int SLOTS>
+// The raw elements come in with cp.async, NST items ahead of their conversion, into stages whose every piece is read by the
+// lane that copied it (8 or 16 bytes: a unit of 16 elements); a row's scale bytes by the lane that looks after the row.
+template <int FMT, int D, int ROWS_K, int VC, bool SPARSE, int NLW, int SLOTS, int NST>
 struct MxLoader {
   static constexpr int KU = D / 16, VU = VC / 16;                      // units per row
   static constexpr int K_RPI = 32 / KU, V_RPI = 32 / VU;               // rows per warp instruction
   static constexpr int K_GROUPS = ROWS_K / (K_RPI * NLW), V_GROUPS = 128 / (V_RPI * NLW);     // row groups of this warp
-  static constexpr int SUB = 4;                                        // of them at a time
-  static constexpr int KSUB = K_GROUPS / SUB, VSUB = V_GROUPS / SUB;
-  static constexpr int K_REGS = (K_GROUPS * K_RPI + 31) / 32, V_REGS = (V_GROUPS * V_RPI + 31) / 32;     // (a lane may be left over)
-  static_assert(K_GROUPS % SUB == 0 && V_GROUPS % SUB == 0 && (KSUB + VSUB) % 2 == 0, "whole groups, alternating buffers");
-  // a row's number, its offset in units of 16 elements (kNoRow: no such row) and its scale bytes; lane l looks after rows p = l, 32 + l
-  // of this warp's rows, p = group * rows per instruction + row of the instruction
-  template <int R> struct Rows { int t[R]; uint32_t off[R], scale[R]; };
+  static constexpr int K_ROWS = K_GROUPS * K_RPI, V_ROWS = V_GROUPS * V_RPI;                  // rows of this warp, a lane each
+  static constexpr int kUnitBytes = 2 * kMxBits<FMT>;
+  static constexpr int kGroups = K_GROUPS > V_GROUPS ? K_GROUPS : V_GROUPS;
+  static constexpr uint32_t kWarpRaw = kGroups * 32 * kUnitBytes;      // a stage: this warp's units, then 32 scale words
+  static constexpr uint32_t kWarpStage = kWarpRaw + 128;
+  static constexpr uint32_t kStageBytes = NST * NLW * kWarpStage;      // shared memory of all of them
+  static_assert(K_ROWS <= 32 && V_ROWS <= 32 && K_GROUPS >= 1 && V_GROUPS >= 1, "a lane per row");
   typedef decltype(MxUnit<FMT>::w) W;
+  // One of the two streams of items: the tile that is copied next, the row number of this lane's row in it (-1: none)
+  struct Stream { int tile, t; };
 
   const DevParams& P;
   int s, kv, lw, lane, k_row0, v_col0, T;
-  uint32_t head, st, sb, srow0;
+  uint32_t head, st, sb, srow0, stage0;              // stage0: shared-memory address of this warp's first stage
   const int32_t *table, *idx;
   const W *kc, *vc;
   int* v_nan;
 
   __device__ __forceinline__ MxLoader(const DevParams& P_, int s_, int kv_, int lw_, int lane_, int k_row0_, int v_col0_, int T_, const void* k,
-                                      const void* v, const int32_t* k_idx, int* v_nan_)
+                                      const void* v, const int32_t* k_idx, int* v_nan_, unsigned char* stages)
       : P(P_), s(s_), kv(kv_), lw(lw_), lane(lane_), k_row0(k_row0_), v_col0(v_col0_), T(T_), v_nan(v_nan_) {
     // (the host refuses caches of 2^32 - 1 units or rows and more)
     st = (uint32_t)(P.kv_st >> 4);
@@ -103,33 +109,32 @@ struct MxLoader {
     idx = SPARSE ? k_idx + ((long long)s * P.n_kv + kv) * P.budget_cap : nullptr;
     kc = static_cast<const W*>(k);
     vc = static_cast<const W*>(v);
+    stage0 = smem_u32(stages) + (uint32_t)lw * (NST * kWarpStage);
   }
 
-  template <bool V> __device__ __forceinline__ int tile_row(int r) const {
+  // this lane's row in a tile (of K: in the whole tile, not the item)
+  template <bool V> __device__ __forceinline__ int tile_row() const {
     constexpr int RPI = V ? V_RPI : K_RPI;
-    const int p = 32 * r + lane;
-    return (V ? 0 : k_row0) + (lw + p / RPI * NLW) * RPI + p % RPI;
+    return (V ? 0 : k_row0) + (lw + lane / RPI * NLW) * RPI + lane % RPI;
   }
-  // row numbers of tile tr (-1 past its end); listed ones are loads
-  template <bool V, int R> __device__ __forceinline__ void numbers(const TileRows& tr, int (&t)[R]) const {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const int rr = 32 * r + lane < (V ? V_GROUPS * V_RPI : K_GROUPS * K_RPI) ? tile_row<V>(r) : 128;
-      if (SPARSE && tr.from_list) {
-        const int last = min(tr.count, kKeyTile) - 1;
-        const int n = last >= 0 ? __ldcg(idx + tr.first + min(rr, last)) : -1;     // written by the kernel before: L2
-        t[r] = rr <= last ? n : -1;
-      } else {
-        t[r] = rr < min(tr.count, kKeyTile) ? tr.first + rr : -1;
-      }
+  // its number in the cache; of a listed one a load
+  template <bool V> __device__ __forceinline__ int number(const AttnGeom& g, int tile) const {
+    const TileRows tr = tile_rows<SPARSE>(g, tile);
+    const int last = min(tr.count, kKeyTile) - 1;
+    const int rr = lane < (V ? V_ROWS : K_ROWS) ? tile_row<V>() : kKeyTile;
+    if (SPARSE && tr.from_list) {
+      const int n = last >= 0 ? __ldcg(idx + tr.first + min(rr, last)) : -1;         // written by the kernel before: L2
+      return rr <= last ? n : -1;
     }
+    return rr <= last ? tr.first + rr : -1;
   }
-  template <bool V, int R> __device__ __forceinline__ void places(const TileRows& tr, Rows<R>& rows) const {
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      int t = rows.t[r];
+  // The copies of the next item of a stream into a stage, one group (empty past the known tiles); then the next row number.
+  template <bool V> __device__ __forceinline__ void copy(const AttnGeom& g, Stream& next, int stage) const {
+    constexpr int GROUPS = V ? V_GROUPS : K_GROUPS, RPI = V ? V_RPI : K_RPI, U = V ? VU : KU;
+    if (next.tile < g.n_known) {
+      int t = next.t;
 #ifdef QUOKA_DEBUG
-      if (SPARSE && tr.from_list && (t < -1 || t >= T)) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
+      if (SPARSE && tile_rows<SPARSE>(g, next.tile).from_list && (t < -1 || t >= T)) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
 #endif
       const int tc = max(t, 0);
       uint32_t off = (uint32_t)tc * st, srow = srow0 + (uint32_t)tc;
@@ -145,135 +150,123 @@ struct MxLoader {
         off = (uint32_t)page * sb + (uint32_t)(tc & (kPage - 1)) * st;
         srow = (uint32_t)page * (uint32_t)(P.n_kv * kPage) + srow0 + (uint32_t)(tc & (kPage - 1));
       }
-      rows.off[r] = t < 0 ? kNoRow : head + off;
-      const uint8_t* sc = (V ? P.v_scale : P.k_scale) + (size_t)srow * (D / kMxBlock);
-      uint32_t w = 0;
-      if (t >= 0) w = D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(sc)) : __ldg(reinterpret_cast<const uint16_t*>(sc));
-      rows.scale[r] = w;
-    }
-  }
-  // the first position that sees a value that is not finite, per block of 32 columns
-  __device__ __forceinline__ void note_nan(const TileRows& tr, const Rows<V_REGS>& rows) const {
-#pragma unroll
-    for (int r = 0; r < V_REGS; ++r)
-      if (rows.off[r] != kNoRow && __vcmpeq4(rows.scale[r], 0xFFFFFFFFu) != 0) {
-#pragma unroll
-        for (int b = 0; b < D / kMxBlock; ++b)
-          if ((rows.scale[r] >> (8 * b) & 0xFFu) == kMxNanScale) atomicMin(v_nan + b, tr.causal ? max(tr.col0 + tile_row<true>(r), -1) : -1);
+      const uint32_t dst = stage0 + (uint32_t)stage * kWarpStage;
+      const uint8_t* sc = (V ? P.v_scale : P.k_scale);
+      if (t >= 0) {
+        if (D == 128) cp_async_4(dst + kWarpRaw + 4 * lane, sc + (size_t)srow * 4);
+        else {
+          const uint32_t w = __ldg(reinterpret_cast<const uint16_t*>(sc) + srow);
+          asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kWarpRaw + 4 * lane), "r"(w) : "memory");
+        }
+      } else {
+        asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kWarpRaw + 4 * lane), "r"(0u) : "memory");
       }
-  }
-  template <bool V, int R> __device__ __forceinline__ void load(const Rows<R>& rows, int sub, W (&buf)[SUB]) const {
-    constexpr int RPI = V ? V_RPI : K_RPI, U = V ? VU : KU;
-    const W* base = (V ? vc : kc) + (V ? (uint32_t)v_col0 >> 4 : 0u) + lane % U;
+      const uint32_t place = t < 0 ? kNoRow : head + off;
+      const W* base = (V ? vc : kc) + (V ? (uint32_t)v_col0 >> 4 : 0u) + lane % U;
 #pragma unroll
-    for (int i = 0; i < SUB; ++i) {
-      const int p = (sub * SUB + i) * RPI;
-      const uint32_t off = __shfl_sync(0xFFFFFFFFu, rows.off[p / 32], (p + lane / U) & 31);
-      W w = {};
-      if (off != kNoRow) w = __ldg(base + off);
-      buf[i] = w;
+      for (int i = 0; i < GROUPS; ++i) {
+        const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, i * RPI + lane / U);
+        cp_async_unit(dst + (uint32_t)(i * 32 + lane) * kUnitBytes, base + (at == kNoRow ? 0u : at), at != kNoRow);
+      }
+      ++next.tile;
+      if (next.tile < g.n_known) next.t = number<V>(g, next.tile);
+    }
+    cp_async_commit();
+  }
+  static __device__ __forceinline__ void cp_async_unit(uint32_t dst, const W* src, bool valid) {
+    if constexpr (kUnitBytes == 16) {
+      cp_async_16(dst, src, valid);
+    } else {
+      const uint32_t n = valid ? 8u : 0u;
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
     }
   }
-  template <bool V, int R> __device__ __forceinline__ void store(const Rows<R>& rows, int sub, const W (&buf)[SUB], unsigned char* item) const {
-    constexpr int RPI = V ? V_RPI : K_RPI, U = V ? VU : KU;
+  // A stage's item as bf16 into the ring; for V, the first position that sees a value that is not finite, per 32 columns.
+  template <bool V> __device__ __forceinline__ void convert(const AttnGeom& g, int tile, int stage, unsigned char* item) const {
+    constexpr int GROUPS = V ? V_GROUPS : K_GROUPS, RPI = V ? V_RPI : K_RPI, U = V ? VU : KU;
     constexpr uint32_t kHalf = (V ? 128 : ROWS_K) * 128;
+    const uint32_t src = stage0 + (uint32_t)stage * kWarpStage;
     const int u = lane % U, rsub = lane / U;
     const int sw = U == 8 ? u >> 2 : 0;               // lanes of the second half store their second piece first: other banks
+    uint32_t mine;
+    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mine) : "r"(src + kWarpRaw + 4 * lane) : "memory");
+    if (V && lane < V_ROWS && __vcmpeq4(mine, 0xFFFFFFFFu) != 0) {
+      const TileRows tr = tile_rows<SPARSE>(g, tile);
 #pragma unroll
-    for (int i = 0; i < SUB; ++i) {
-      const int p = (sub * SUB + i) * RPI;
-      const uint32_t word = __shfl_sync(0xFFFFFFFFu, rows.scale[p / 32], (p + rsub) & 31);
+      for (int b = 0; b < D / kMxBlock; ++b)
+        if ((mine >> (8 * b) & 0xFFu) == kMxNanScale) atomicMin(v_nan + b, tr.causal ? max(tr.col0 + tile_row<true>(), -1) : -1);
+    }
+    W raw[GROUPS];
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const uint32_t at = src + (uint32_t)(i * 32 + lane) * kUnitBytes;
+      if constexpr (FMT == QUOKA_KV_MXFP8)
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw[i].x), "=r"(raw[i].y), "=r"(raw[i].z), "=r"(raw[i].w) : "r"(at) : "memory");
+      else
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(raw[i].x), "=r"(raw[i].y) : "r"(at) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      const uint32_t word = __shfl_sync(0xFFFFFFFFu, mine, i * RPI + rsub);
       const uint32_t b = word >> (8 * ((V ? v_col0 / kMxBlock : 0) + (u >> 1))) & 0xFFu;
       const uint32_t f = b == kMxNanScale ? (V ? 0u : kBf16Nan2) : mx_factor2<FMT>(b);
-      const int row = (lw + (sub * SUB + i) * NLW) * RPI + rsub;
+      const int row = (lw + i * NLW) * RPI + rsub;
       unsigned char* dst = item + (uint32_t)(u >> 2) * kHalf + (uint32_t)row * 128u;
       const uint32_t p0 = (uint32_t)(((2 * (u & 3) + sw) ^ row) & 7) << 4;
       uint4 first, second;
       if constexpr (FMT == QUOKA_KV_MXFP8) {
-        first = mx_to_bf16x8<FMT>(sw ? buf[i].z : buf[i].x, sw ? buf[i].w : buf[i].y, f);
-        second = mx_to_bf16x8<FMT>(sw ? buf[i].x : buf[i].z, sw ? buf[i].y : buf[i].w, f);
+        first = mx_to_bf16x8<FMT>(sw ? raw[i].z : raw[i].x, sw ? raw[i].w : raw[i].y, f);
+        second = mx_to_bf16x8<FMT>(sw ? raw[i].x : raw[i].z, sw ? raw[i].y : raw[i].w, f);
       } else {
-        first = mx_to_bf16x8<FMT>(sw ? buf[i].y : buf[i].x, 0u, f);
-        second = mx_to_bf16x8<FMT>(sw ? buf[i].x : buf[i].y, 0u, f);
+        first = mx_to_bf16x8<FMT>(sw ? raw[i].y : raw[i].x, 0u, f);
+        second = mx_to_bf16x8<FMT>(sw ? raw[i].x : raw[i].y, 0u, f);
       }
       *reinterpret_cast<uint4*>(dst + p0) = first;
       *reinterpret_cast<uint4*>(dst + (p0 ^ 16u)) = second;
     }
   }
 
-  // All tiles of this CTA's walk; false when a wait gave up.
+  // All tiles of this CTA's walk (until a wait gives up).
   template <typename Learn>
-  __device__ __forceinline__ bool run(AttnGeom& g, int t_lo, unsigned char* ring, uint32_t slot_bytes, uint64_t* full, uint64_t* empty,
+  __device__ __forceinline__ void run(AttnGeom& g, int t_lo, unsigned char* ring, uint32_t slot_bytes, uint64_t* full, uint64_t* empty,
                                       const WaitCtx& wc, Learn&& learn) {
-    int tile = t_lo, slot = 0;
+    int tile = t_lo, slot = 0, stage = 0;
     uint32_t phase = 0;
-    if (tile == g.n_known) {
-      if (!g.resolved) learn();
-      if (tile == g.n_known) return true;
-    }
-    Rows<K_REGS> k;
-    Rows<V_REGS> v;
-    W buf[2][SUB];
-    TileRows tr = tile_rows<SPARSE>(g, tile);
-    const auto whole = [&]() {                        // everything about tile tr, and its first loads
-      numbers<false>(tr, k.t);
-      numbers<true>(tr, v.t);
-      places<false>(tr, k);
-      places<true>(tr, v);
-      load<false>(k, 0, buf[0]);
+    Stream k{t_lo, -1}, v{t_lo, -1};
+    const auto one = [&](auto is_v) -> bool {         // the next item: conversion, and copies into the stage it leaves
+      constexpr bool V = decltype(is_v)::value;
+      cp_async_wait<NST - 1>();
+      __syncwarp();
+      if (!mbar_wait_done(&empty[slot], phase ^ 1, wc)) return false;
+      convert<V>(g, tile, stage, ring + (size_t)slot * slot_bytes);
+      fence_proxy_async_smem();                       // these stores, before products read the slot
+      __syncwarp();
+      if (lane == 0) mbar_arrive(&full[slot]);
+      if (++slot == SLOTS) { slot = 0; phase ^= 1; }
+      if constexpr (NST % 2 == 0) copy<V>(g, V ? v : k, stage);
+      else copy<!V>(g, V ? k : v, stage);
+      if (++stage == NST) stage = 0;
+      return true;
     };
-    whole();
     for (;;) {
-      const bool next = tile + 1 < g.n_known;
-      TileRows tn = tr;
-      int kt[K_REGS], vt[V_REGS];
-      if (next) {
-        tn = tile_rows<SPARSE>(g, tile + 1);
-        numbers<false>(tn, kt);
-        numbers<true>(tn, vt);
-      }
-      note_nan(tr, v);
-#pragma unroll
-      for (int sub = 0; sub < KSUB + VSUB; ++sub) {
-        // the next group's loads, then this one's conversion; a K tile of the next row numbers behind the last V group
-        if (sub + 1 == KSUB + VSUB) {
-          if (next) {
-#pragma unroll
-            for (int r = 0; r < K_REGS; ++r) k.t[r] = kt[r];
-            places<false>(tn, k);
-            load<false>(k, 0, buf[(sub + 1) & 1]);
-          }
-        } else if (sub + 1 < KSUB) {
-          load<false>(k, sub + 1, buf[(sub + 1) & 1]);
-        } else {
-          load<true>(v, sub + 1 - KSUB, buf[(sub + 1) & 1]);
-        }
-        if (sub == 0 || sub == KSUB)
-          if (!mbar_wait_done(&empty[slot], phase ^ 1, wc)) return false;
-        unsigned char* item = ring + (size_t)slot * slot_bytes;
-        if (sub < KSUB) store<false>(k, sub, buf[sub & 1], item);
-        else store<true>(v, sub - KSUB, buf[sub & 1], item);
-        if (sub == KSUB - 1 || sub == KSUB + VSUB - 1) {
-          fence_proxy_async_smem();                   // these stores, before products read the slot
-          __syncwarp();
-          if (lane == 0) mbar_arrive(&full[slot]);
-          if (++slot == SLOTS) { slot = 0; phase ^= 1; }
-        }
-      }
-      ++tile;
-      if (next) {
-#pragma unroll
-        for (int r = 0; r < V_REGS; ++r) v.t[r] = vt[r];
-        tr = tn;
-        places<true>(tr, v);
-      } else {
-        if (g.resolved) return true;
+      if (tile == g.n_known) {                        // end of what is known: the list length, or the end
+        if (g.resolved) break;
         learn();
-        if (tile == g.n_known) return true;
-        tr = tile_rows<SPARSE>(g, tile);
-        whole();
+        if (tile == g.n_known) break;
       }
+      k.tile = v.tile = tile;                         // (all copies have been converted)
+      k.t = number<false>(g, tile);
+      v.t = number<true>(g, tile);
+#pragma unroll
+      for (int i = 0; i < NST; ++i) {
+        const int at = stage + i < NST ? stage + i : stage + i - NST;
+        if (i % 2 == 0) copy<false>(g, k, at); else copy<true>(g, v, at);
+      }
+      for (; tile < g.n_known; ++tile)
+        if (!one(std::false_type{}) || !one(std::true_type{})) goto out;
     }
+  out:
+    cp_async_wait_all();                              // nothing of this thread is in flight at exit
   }
 };
 

@@ -286,7 +286,7 @@ quoka_status launch_attn_tc(const quoka_params* p, const DevParams& P0, const vo
   if (!encode_kv_tensor_map(&tm_k, p, k, 64) || !encode_kv_tensor_map(&tm_v, p, v, 64)) return QUOKA_ERR_CUDA;
   const bool wide = P.d == 128;
   return launch_attn_plan(p, P, plan, wide ? pick_attn_tc<128, 0> : pick_attn_tc<64, 0>, "attn_tc", /*cluster=*/1, kAttnThreads,
-                          wide ? kAttnSmem<128> : kAttnSmem<64>, tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse, st, after_selection);
+                          wide ? attn_tc_smem<128>() : attn_tc_smem<64>(), tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse, st, after_selection);
 }
 
 }  // namespace quoka

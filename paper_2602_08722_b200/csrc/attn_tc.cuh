@@ -29,10 +29,16 @@
 
 namespace quoka {
 
-template <int D>
-constexpr int kSlotsOf = D == 64 ? 8 : 5;                    // of 16 KB, 32 KB
-template <int D>
-constexpr size_t kAttnSmem = 1024 + (size_t)(2 + kSlotsOf<D>) * (D / 64) * 16384 + 512;
+template <int D, int FMT = 0>
+constexpr int kSlotsOf = D == 64 ? 8 : FMT == 0 ? 5 : 4;     // of 16 KB, 32 KB
+template <int D, int FMT, bool SPARSE>
+using MxTileLoader = MxLoader<FMT, D, 128, D, SPARSE, kMxLoaderWarps, kSlotsOf<D, FMT>, D == 128 && FMT == QUOKA_KV_MXFP8 ? 2 : 3>;
+template <int D, int FMT = 0>
+constexpr size_t attn_tc_smem() {
+  size_t n = 1024 + (size_t)(2 + kSlotsOf<D, FMT>) * (D / 64) * 16384 + 512;
+  if constexpr (FMT != 0) n += MxTileLoader<D, FMT, false>::kStageBytes;
+  return n;
+}
 
 template <int D, bool SPARSE, bool SPLIT, int FMT = 0>
 __global__ void __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1)
@@ -40,7 +46,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
                const __grid_constant__ CUtensorMap tm_v, const __nv_bfloat16* __restrict__ kc,
                const __nv_bfloat16* __restrict__ vc, const int32_t* __restrict__ k_idx,
                const int32_t* __restrict__ k_cnt, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
-  constexpr int kSlots = kSlotsOf<D>, HALVES = D / 64;
+  constexpr int kSlots = kSlotsOf<D, FMT>, HALVES = D / 64;
   constexpr bool MX = FMT != 0;                              // a microscaled cache: kc, vc are its bytes
   constexpr int kThreads = MX ? kMxAttnThreads : kAttnThreads;
   constexpr uint32_t kHalfBytes = 128 * 128;                 // 128 rows x 128 B
@@ -173,7 +179,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     // One warp instruction copies four whole rows (eight lanes x 16 bytes cover a 128-byte row; head_dim 128: two); the row
     // groups of a tile are dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxLoader<FMT, D, 128, D, SPARSE, kMxLoaderWarps, kSlots> loader(P, s, kv, warp - kMxFirstLoader, lane, 0, 0, g.T, kc, vc, k_idx, v_nan);
+      MxTileLoader<D, FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 0, 0, g.T, kc, vc, k_idx, v_nan, reinterpret_cast<unsigned char*>(bars) + 512);
       loader.run(g, t_lo, kv_smem, kTileBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;

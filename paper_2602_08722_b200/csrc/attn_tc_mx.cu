@@ -31,8 +31,11 @@ quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P0, int f
   AttnKernel (*const kernel)(bool, bool, bool) = pair ? (fp8 ? pick<true, true, true> : pick<true, true, false>)
                                                  : wide ? (fp8 ? pick<false, true, true> : pick<false, true, false>)
                                                         : (fp8 ? pick<false, false, true> : pick<false, false, false>);
+  const size_t smem = pair ? (fp8 ? attn_tc_pair_smem<QUOKA_KV_MXFP8>(plan) : attn_tc_pair_smem<QUOKA_KV_MXFP4>(plan))
+                      : wide ? (fp8 ? attn_tc_smem<128, QUOKA_KV_MXFP8>() : attn_tc_smem<128, QUOKA_KV_MXFP4>())
+                             : (fp8 ? attn_tc_smem<64, QUOKA_KV_MXFP8>() : attn_tc_smem<64, QUOKA_KV_MXFP4>());
   return launch_attn_plan(p, P, plan, kernel, pair ? "attn_tc_pair_mx" : "attn_tc_mx", pair ? 2 : 1, kMxAttnThreads,
-                          pair ? attn_tc_pair_smem(plan) : wide ? kAttnSmem<128> : kAttnSmem<64>, tm_q, none, none, k, v, k_idx, k_cnt, out, lse, st,
+                          smem, tm_q, none, none, k, v, k_idx, k_cnt, out, lse, st,
                           after_selection);
 }
 

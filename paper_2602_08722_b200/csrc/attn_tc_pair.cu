@@ -10,7 +10,7 @@ quoka_status launch_attn_tc_pair(const quoka_params* p, const DevParams& P, cons
   if (!encode_q_tensor_map(&tm_q, P, q)) return QUOKA_ERR_CUDA;
   CUtensorMap tm_k, tm_v;
   if (!encode_kv_tensor_map(&tm_k, p, k, 64) || !encode_kv_tensor_map(&tm_v, p, v, 64)) return QUOKA_ERR_CUDA;
-  return launch_attn_plan(p, P, plan, pick_attn_tc_pair<0>, "attn_tc_pair", /*cluster=*/2, kAttnThreads, attn_tc_pair_smem(plan), tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse,
+  return launch_attn_plan(p, P, plan, pick_attn_tc_pair<0>, "attn_tc_pair", /*cluster=*/2, kAttnThreads, attn_tc_pair_smem<0>(plan), tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse,
                           st, after_selection);
 }
 

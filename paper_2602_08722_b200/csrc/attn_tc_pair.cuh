@@ -36,6 +36,9 @@ constexpr int kPairLoaderWarps = kLoaderWarps;
 constexpr uint32_t kPairSlotBytes = 16384;
 constexpr uint32_t kPairQTileBytes = 32768;
 
+template <int FMT, bool SPARSE>
+using MxPairLoader = MxLoader<FMT, 128, 64, 64, SPARSE, kMxLoaderWarps, kPairSlots, 3>;
+
 enum { kWhole = 0, kParts = 1, kPartsCluster = 2 };     // a row block per pair; parts merged through memory / in a cluster
 
 template <bool SPARSE, int MODE, int FMT = 0>
@@ -193,7 +196,8 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     // V item: all 128 tile rows, bytes [128 * rank, 128 * rank + 128) of each (8 pieces, 4 rows per instruction).
     // Either way an item is 32 row groups, dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxLoader<FMT, D, 64, 64, SPARSE, kMxLoaderWarps, kPairSlots> loader(P, s, kv, warp - kMxFirstLoader, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan);
+      MxPairLoader<FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan,
+                                       reinterpret_cast<unsigned char*>(bars) + 512 + (MODE == kPartsCluster ? 2048 : 0));
       loader.run(g, t_lo, kv_smem, kPairSlotBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;
@@ -432,8 +436,11 @@ AttnKernel pick_attn_tc_pair(bool sparse, bool parts, bool in_cluster) {
   if (parts) return sparse ? attn_tc_pair_kernel<true, true, FMT> : attn_tc_pair_kernel<false, true, FMT>;
   return sparse ? attn_tc_pair_kernel<true, false, FMT> : attn_tc_pair_kernel<false, false, FMT>;
 }
-inline size_t attn_tc_pair_smem(const AttnPlan& plan) {
-  return 1024 + 2 * kPairQTileBytes + (size_t)kPairSlots * kPairSlotBytes + 512 + (plan.in_cluster ? 2048 : 0);
+template <int FMT>
+size_t attn_tc_pair_smem(const AttnPlan& plan) {
+  size_t n = 1024 + 2 * kPairQTileBytes + (size_t)kPairSlots * kPairSlotBytes + 512 + (plan.in_cluster ? 2048 : 0);
+  if constexpr (FMT != 0) n += MxPairLoader<FMT, false>::kStageBytes;
+  return n;
 }
 
 }  // namespace quoka
