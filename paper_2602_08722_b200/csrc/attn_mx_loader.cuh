@@ -82,13 +82,14 @@ struct MxLoader {
   static constexpr int K_ROWS = K_GROUPS * K_RPI, V_ROWS = V_GROUPS * V_RPI;                  // rows of this warp, a lane each
   static constexpr int kUnitBytes = 2 * kMxBits<FMT>;
   static constexpr int kGroups = K_GROUPS > V_GROUPS ? K_GROUPS : V_GROUPS;
-  static constexpr uint32_t kWarpRaw = kGroups * 32 * kUnitBytes;      // a stage: this warp's units, then 32 scale words
-  static constexpr uint32_t kWarpStage = kWarpRaw + 128;
+  static constexpr uint32_t kWarpRaw = kGroups * 32 * kUnitBytes;      // a stage: this warp's units, 32 scale words, their shifts
+  static constexpr uint32_t kWarpStage = kWarpRaw + (D == 128 ? 128 : 256);
   static constexpr uint32_t kStageBytes = NST * NLW * kWarpStage;      // shared memory of all of them
   static_assert(K_ROWS <= 32 && V_ROWS <= 32 && K_GROUPS >= 1 && V_GROUPS >= 1, "a lane per row");
   typedef decltype(MxUnit<FMT>::w) W;
-  // One of the two streams of items: the tile that is copied next, the row number of this lane's row in it (-1: none)
-  struct Stream { int tile, t; };
+  // One of the two streams of items: the tile that is copied next, and the number of this lane's row in it (if it has one; looked
+  // at only when the copies are issued, an item later than it is asked for)
+  struct Stream { int tile, n; };
 
   const DevParams& P;
   int s, kv, lw, lane, k_row0, v_col0, T;
@@ -120,19 +121,19 @@ struct MxLoader {
   // its number in the cache; of a listed one a load
   template <bool V> __device__ __forceinline__ int number(const AttnGeom& g, int tile) const {
     const TileRows tr = tile_rows<SPARSE>(g, tile);
-    const int last = min(tr.count, kKeyTile) - 1;
-    const int rr = lane < (V ? V_ROWS : K_ROWS) ? tile_row<V>() : kKeyTile;
-    if (SPARSE && tr.from_list) {
-      const int n = last >= 0 ? __ldcg(idx + tr.first + min(rr, last)) : -1;         // written by the kernel before: L2
-      return rr <= last ? n : -1;
-    }
-    return rr <= last ? tr.first + rr : -1;
+    const int rr = tile_row<V>();
+    if (SPARSE && tr.from_list) return __ldcg(idx + tr.first + max(min(rr, min(tr.count, kKeyTile) - 1), 0));    // written by the kernel before: L2
+    return tr.first + rr;
+  }
+  // whether there is such a row
+  template <bool V> __device__ __forceinline__ bool exists(const AttnGeom& g, int tile) const {
+    return lane < (V ? V_ROWS : K_ROWS) && tile_row<V>() < min(tile_rows<SPARSE>(g, tile).count, kKeyTile);
   }
   // The copies of the next item of a stream into a stage, one group (empty past the known tiles); then the next row number.
   template <bool V> __device__ __forceinline__ void copy(const AttnGeom& g, Stream& next, int stage) const {
     constexpr int GROUPS = V ? V_GROUPS : K_GROUPS, RPI = V ? V_RPI : K_RPI, U = V ? VU : KU;
     if (next.tile < g.n_known) {
-      int t = next.t;
+      int t = exists<V>(g, next.tile) ? next.n : -1;
 #ifdef QUOKA_DEBUG
       if (SPARSE && tile_rows<SPARSE>(g, next.tile).from_list && (t < -1 || t >= T)) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
 #endif
@@ -153,14 +154,12 @@ struct MxLoader {
       const uint32_t dst = stage0 + (uint32_t)stage * kWarpStage;
       const uint8_t* sc = (V ? P.v_scale : P.k_scale);
       if (t >= 0) {
-        if (D == 128) cp_async_4(dst + kWarpRaw + 4 * lane, sc + (size_t)srow * 4);
-        else {
-          const uint32_t w = __ldg(reinterpret_cast<const uint16_t*>(sc) + srow);
-          asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kWarpRaw + 4 * lane), "r"(w) : "memory");
-        }
+        // (head_dim 64: the word that has the scales of two rows)
+        cp_async_4(dst + kWarpRaw + 4 * lane, sc + (D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4));
       } else {
         asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kWarpRaw + 4 * lane), "r"(0u) : "memory");
       }
+      if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(dst + kWarpRaw + 128 + 4 * lane), "r"((srow & 1u) * 16) : "memory");
       const uint32_t place = t < 0 ? kNoRow : head + off;
       const W* base = (V ? vc : kc) + (V ? (uint32_t)v_col0 >> 4 : 0u) + lane % U;
 #pragma unroll
@@ -169,7 +168,7 @@ struct MxLoader {
         cp_async_unit(dst + (uint32_t)(i * 32 + lane) * kUnitBytes, base + (at == kNoRow ? 0u : at), at != kNoRow);
       }
       ++next.tile;
-      if (next.tile < g.n_known) next.t = number<V>(g, next.tile);
+      if (next.tile < g.n_known) next.n = number<V>(g, next.tile);
     }
     cp_async_commit();
   }
@@ -190,6 +189,11 @@ struct MxLoader {
     const int sw = U == 8 ? u >> 2 : 0;               // lanes of the second half store their second piece first: other banks
     uint32_t mine;
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(mine) : "r"(src + kWarpRaw + 4 * lane) : "memory");
+    if (D == 64) {
+      uint32_t shift;
+      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(src + kWarpRaw + 128 + 4 * lane) : "memory");
+      mine = mine >> shift & 0xFFFFu;
+    }
     if (V && lane < V_ROWS && __vcmpeq4(mine, 0xFFFFFFFFu) != 0) {
       const TileRows tr = tile_rows<SPARSE>(g, tile);
 #pragma unroll
@@ -255,8 +259,8 @@ struct MxLoader {
         if (tile == g.n_known) break;
       }
       k.tile = v.tile = tile;                         // (all copies have been converted)
-      k.t = number<false>(g, tile);
-      v.t = number<true>(g, tile);
+      k.n = number<false>(g, tile);
+      v.n = number<true>(g, tile);
 #pragma unroll
       for (int i = 0; i < NST; ++i) {
         const int at = stage + i < NST ? stage + i : stage + i - NST;
