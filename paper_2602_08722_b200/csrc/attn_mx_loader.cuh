@@ -11,7 +11,7 @@
 // column set it to minus infinity.  A value's block becomes zeros, as its products with weights of zero would reach rows that do not see
 // it; the first chunk position that sees one is kept per block of columns, and the epilogue makes NaN of what is at or behind it.
 //
-// What bounds it: instructions.  Five a pair of elements, 16 elements a lane and copy; copies run two or three
+// What bounds it: instructions, about four a pair of elements; copies run two or three
 // items ahead of the conversion.
 #pragma once
 
@@ -47,27 +47,45 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
   return d;
 }
-// Elements whose bits stand at the top of each half of h, as bf16 numbers times 2^-120 or 2^-126.
-template <int FMT>
-__device__ __forceinline__ uint32_t mx_spread(uint32_t h) {
-  if constexpr (FMT == QUOKA_KV_MXFP8) return (h & 0x80008000u) | (h >> 4 & 0x07F007F0u);
-  else return (h & 0x80008000u) | (h >> 6 & 0x01C001C0u);
-}
-// The 8 elements of half a unit (two words of MXFP8, one of MXFP4) as four bf16 pairs.
+// The 8 elements of half a unit (two words of MXFP8, one of MXFP4) as four bf16 pairs, in the order in which their bits are reached by
+// shifts and masks alone: 0 2 1 3 4 6 5 7, or 0 4 1 5 2 6 3 7 (mx_place).  Queries are put in the same order once per CTA, so that products
+// are the same; the columns of O come out in it, and the epilogues take them from there.  Against the plain order, by byte
+// permutations, it saves a third of the conversion's instructions on the integer pipe, which the softmax warps need too.
 template <int FMT>
 __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t factor2) {
   uint32_t o[4];
   if constexpr (FMT == QUOKA_KV_MXFP8) {
-    o[0] = __byte_perm(w0, w0, 0x1100); o[1] = __byte_perm(w0, w0, 0x3322);
-    o[2] = __byte_perm(w1, w1, 0x1100); o[3] = __byte_perm(w1, w1, 0x3322);
+    o[0] = (w0 << 8 & 0x80008000u) | (w0 << 4 & 0x07F007F0u);
+    o[1] = (w0 & 0x80008000u) | (w0 >> 4 & 0x07F007F0u);
+    o[2] = (w1 << 8 & 0x80008000u) | (w1 << 4 & 0x07F007F0u);
+    o[3] = (w1 & 0x80008000u) | (w1 >> 4 & 0x07F007F0u);
   } else {
-    const uint32_t lo = w0 << 4;                     // (what stands below an element's bits is masked off)
-    o[0] = __byte_perm(lo, w0, 0x4400); o[1] = __byte_perm(lo, w0, 0x5511);
-    o[2] = __byte_perm(lo, w0, 0x6622); o[3] = __byte_perm(lo, w0, 0x7733);
+    o[0] = (w0 << 12 & 0x80008000u) | (w0 << 6 & 0x01C001C0u);
+    o[1] = (w0 << 8 & 0x80008000u) | (w0 << 2 & 0x01C001C0u);
+    o[2] = (w0 << 4 & 0x80008000u) | (w0 >> 2 & 0x01C001C0u);
+    o[3] = (w0 & 0x80008000u) | (w0 >> 6 & 0x01C001C0u);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = mul_bf16x2(mx_spread<FMT>(o[i]), factor2);
+  for (int i = 0; i < 4; ++i) o[i] = mul_bf16x2(o[i], factor2);
   return make_uint4(o[0], o[1], o[2], o[3]);
+}
+// 8 bf16 numbers in plain order, put in that order.
+template <int FMT>
+__device__ __forceinline__ uint4 mx_order(uint4 w) {
+  const uint32_t a = FMT == QUOKA_KV_MXFP8 ? w.y : w.z, b = FMT == QUOKA_KV_MXFP8 ? w.z : w.y;     // what goes with x, and with w
+  return make_uint4(__byte_perm(w.x, a, 0x5410), __byte_perm(w.x, a, 0x7632), __byte_perm(b, w.w, 0x5410), __byte_perm(b, w.w, 0x7632));
+}
+// The CTA's Q tiles in that order, in place: by the loader warps, behind their first copies; `ready` gets an arrival of each warp.
+template <int FMT>
+__device__ __forceinline__ bool mx_order_q(unsigned char* q_smem, int bytes, int thread, int threads, uint64_t* q_full, uint64_t* ready, const WaitCtx& wc) {
+  if (!mbar_wait(q_full, 0, wc)) return false;
+  uint4* q = reinterpret_cast<uint4*>(q_smem);
+#pragma unroll 4
+  for (int i = thread; i < bytes / 16; i += threads) q[i] = mx_order<FMT>(q[i]);
+  fence_proxy_async_smem();
+  __syncwarp();
+  if ((thread & 31) == 0) mbar_arrive(ready);
+  return true;
 }
 
 // One loader warp of NLW.  A K item of the ring is ROWS_K tile rows from row k_row0 on, all D columns; a V item all 128 rows, VC columns
@@ -231,9 +249,10 @@ struct MxLoader {
   }
 
   // All tiles of this CTA's walk (until a wait gives up).
-  template <typename Learn>
+  template <typename Learn, typename Begun>
   __device__ __forceinline__ void run(AttnGeom& g, int t_lo, unsigned char* ring, uint32_t slot_bytes, uint64_t* full, uint64_t* empty,
-                                      const WaitCtx& wc, Learn&& learn) {
+                                      const WaitCtx& wc, Learn&& learn, Begun&& begun) {
+    bool first = true;
     int tile = t_lo, slot = 0, stage = 0;
     uint32_t phase = 0;
     Stream k{t_lo, -1}, v{t_lo, -1};
@@ -254,9 +273,11 @@ struct MxLoader {
     };
     for (;;) {
       if (tile == g.n_known) {                        // end of what is known: the list length, or the end
-        if (g.resolved) break;
-        learn();
-        if (tile == g.n_known) break;
+        if (!g.resolved) learn();
+        if (tile == g.n_known) {
+          if (first) begun();                         // (a part without tiles)
+          break;
+        }
       }
       k.tile = v.tile = tile;                         // (all copies have been converted)
       k.n = number<false>(g, tile);
@@ -266,6 +287,8 @@ struct MxLoader {
         const int at = stage + i < NST ? stage + i : stage + i - NST;
         if (i % 2 == 0) copy<false>(g, k, at); else copy<true>(g, v, at);
       }
+      if (first && !begun()) break;
+      first = false;
       for (; tile < g.n_known; ++tile)
         if (!one(std::false_type{}) || !one(std::true_type{})) goto out;
     }

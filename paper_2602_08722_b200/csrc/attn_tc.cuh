@@ -66,7 +66,8 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
   uint64_t* p_done = p_full + 2 * NBUF;     // [NBUF]    MMA commit: P has been multiplied, the buffer is free
   uint64_t* o_full = p_done + NBUF;         // [2]       MMA commit after the last PV
   uint64_t* q_full = o_full + 2;            // TMA
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_full + 1);
+  uint64_t* q_ready = q_full + 1;           // MX: the Q tiles are in the order of the converted rows, 4 loader warps
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 1);
   __shared__ int abort_flag;
   __shared__ int v_nan[D / kMxBlock];       // MX
 
@@ -99,6 +100,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     for (int i = 0; i < 2 * NBUF; ++i) mbar_init(&p_full[i], 4);
     for (int i = 0; i < 2; ++i) mbar_init(&o_full[i], 1);
     mbar_init(q_full, 1);
+    mbar_init(q_ready, kMxLoaderWarps);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
     if constexpr (MX) {
@@ -165,12 +167,12 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     if constexpr (!SPLIT) {
       if (ok && active_x && mbar_wait(&o_full[x], 0, wc)) {
         tc_fence_after();
-        attn_store_row<D, MX>(P, o_addr, m_run, l_run, s, qr.head(P, row_in_tile), row, row_in_tile < qr.count(P, x), out, lse, v_nan);
+        attn_store_row<D, FMT>(P, o_addr, m_run, l_run, s, qr.head(P, row_in_tile), row, row_in_tile < qr.count(P, x), out, lse, v_nan);
       }
     } else {
       const bool have = ok && active_x && mbar_wait(&o_full[x], 0, wc);
       if (have) tc_fence_after();
-      attn_split_epilogue<D, MX>(P, (s * QRows::groups(P) + hg) * P.attn_split_rb + rb, blockIdx.y % n_parts, n_parts, x, quarter, lane,
+      attn_split_epilogue<D, FMT>(P, (s * QRows::groups(P) + hg) * P.attn_split_rb + rb, blockIdx.y % n_parts, n_parts, x, quarter, lane,
                              row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s, qr.head(P, row_in_tile),
                              out, lse, v_nan);
     }
@@ -180,7 +182,9 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     // groups of a tile are dealt round-robin to the loader warps.
     if constexpr (MX) {
       MxTileLoader<D, FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 0, 0, g.T, kc, vc, k_idx, v_nan, reinterpret_cast<unsigned char*>(bars) + 512);
-      loader.run(g, t_lo, kv_smem, kTileBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
+      loader.run(g, t_lo, kv_smem, kTileBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); }, [&]() {
+        return mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc);
+      });
     } else {
     const int lw = warp - 8;
     constexpr int PIECES = D / 8;                             // 16-byte pieces per row (16 or 8)
@@ -325,7 +329,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
       const uint32_t idesc_qk = idesc_bf16_f32(128, kKeyTile, false, false);
       const uint64_t desc_q = smem_desc_sw128(smem_u32(q_smem), 16, 1024);
       const uint64_t desc_k = smem_desc_sw128(kv_base, 16, 1024);            // K-major rows (K tiles)
-      if (warp_all(mbar_poll(q_full, 0, wc)))
+      if (warp_all(mbar_poll(MX ? q_ready : q_full, 0, wc)))
         attn_issue_qk<NBUF, kSlots>(
             g, t_lo, [&]() { resolve(g, k_cnt, s); uniform_geom(g); grid_launch_dependents(); }, acquire,
             [&](unsigned buf, uint32_t parity) {

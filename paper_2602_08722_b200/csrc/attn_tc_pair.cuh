@@ -67,7 +67,8 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
   uint64_t* o_full = p_done + 2;                  // [2]           MMA commit (both CTAs)
   uint64_t* q_full = o_full + 2;                  // this CTA's Q tiles (TMA)
   uint64_t* peer_q = q_full + 1;                  // first CTA only: the second CTA's Q tiles have landed
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(peer_q + 1);
+  uint64_t* q_ready = peer_q + 1;                 // MX: this CTA's Q tiles are in the order of the converted rows, 4 loader warps
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 1);
   float* part_ml = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);   // [2][m | l][128], kPartsCluster
   __shared__ int abort_flag;
   __shared__ int v_nan[D / kMxBlock];             // MX
@@ -98,6 +99,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     mbar_init(s_free, 8);
     mbar_init(q_full, 1);
     mbar_init(peer_q, 1);
+    mbar_init(q_ready, kMxLoaderWarps);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
     if constexpr (MX) {
@@ -174,7 +176,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     if constexpr (!SPLIT) {
       if (ok && active_x && mbar_wait(&o_full[x], 0, wc)) {
         tc_fence_after();
-        attn_store_row<D, MX>(P, o_addr, m_run, l_run, s, qr.head(P, row_in_tile), row, row_in_tile < qr.count(P, x), out, lse, v_nan);
+        attn_store_row<D, FMT>(P, o_addr, m_run, l_run, s, qr.head(P, row_in_tile), row, row_in_tile < qr.count(P, x), out, lse, v_nan);
       }
     } else if constexpr (MODE == kPartsCluster) {
       // every product of the CTA has been formed when both are final: the ring and the Q tiles are free
@@ -182,11 +184,11 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
       bool have = ok && active_x && mbar_wait(&o_full[x], 0, wc);
       if (have && other) have = mbar_wait(&o_full[x ^ 1], 0, wc);
       if (have) tc_fence_after();
-      attn_part_to_smem<D, MX>(smem, part_ml, x, row_in_tile, have, o_addr, m_run, l_run, row, v_nan);
+      attn_part_to_smem<D, FMT>(smem, part_ml, x, row_in_tile, have, o_addr, m_run, l_run, row, v_nan);
     } else {
       const bool have = ok && active_x && mbar_wait(&o_full[x], 0, wc);
       if (have) tc_fence_after();
-      attn_split_epilogue<D, MX>(P, ((s * QRows::groups(P) + hg) * P.attn_split_rb + rb) * 2 + (int)rank, blockIdx.y % n_parts, n_parts, x,
+      attn_split_epilogue<D, FMT>(P, ((s * QRows::groups(P) + hg) * P.attn_split_rb + rb) * 2 + (int)rank, blockIdx.y % n_parts, n_parts, x,
                              quarter, lane, row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s,
                              qr.head(P, row_in_tile), out, lse, v_nan);
     }
@@ -198,7 +200,9 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     if constexpr (MX) {
       MxPairLoader<FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan,
                                        reinterpret_cast<unsigned char*>(bars) + 512 + (MODE == kPartsCluster ? 2048 : 0));
-      loader.run(g, t_lo, kv_smem, kPairSlotBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); });
+      loader.run(g, t_lo, kv_smem, kPairSlotBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); }, [&]() {
+        return mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kPairQTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc);
+      });
     } else {
     const int lw = warp - 8;
     constexpr int GROUPS = 32;
@@ -317,7 +321,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
       bool ok = true;
       if (warp == kQkWarp) {
         if (!SPLIT) load_q();
-        ok = mbar_wait(q_full, 0, wc);
+        ok = mbar_wait(MX ? q_ready : q_full, 0, wc);
         if (ok) mbar_arrive_cluster(map_to_cta(smem_u32(peer_q), first));
       }
       const uint32_t peer_full0 = map_to_cta(smem_u32(peer_full), first);
@@ -355,7 +359,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     if (warp == kQkWarp) {
       const uint32_t idesc_qk = idesc_bf16_f32(256, kKeyTile, false, false);
       const uint64_t desc_q = smem_desc_sw128(smem_u32(q_smem), 16, 1024);
-      if (warp_all(mbar_poll(q_full, 0, wc) && mbar_poll(peer_q, 0, wc)))
+      if (warp_all(mbar_poll(MX ? q_ready : q_full, 0, wc) && mbar_poll(peer_q, 0, wc)))
         attn_issue_qk<1, kPairSlots>(
             g, t_lo, [&]() { resolve(g, k_cnt, s); uniform_geom(g); grid_launch_dependents(); }, acquire,
             [&](unsigned, uint32_t parity) {
@@ -409,7 +413,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
   tc_fence_before();
   if constexpr (MODE == kPartsCluster) {
     cluster_sync_all();                                       // every part's result is in its shared memory
-    attn_merge_cluster<D, MX>(P, smem, part_ml, warp, kThreads / 32, lane, 2, (int)rank, n_parts, blockIdx.y % n_parts, qr, s, out, lse);
+    attn_merge_cluster<D, FMT>(P, smem, part_ml, warp, kThreads / 32, lane, 2, (int)rank, n_parts, blockIdx.y % n_parts, qr, s, out, lse);
   }
   cluster_sync_all();                                         // the other CTA's MMAs no longer read this CTA
   if (warp == kQkWarp) tmem_dealloc_pair(tmem_base, 512);

@@ -453,39 +453,43 @@ __device__ __forceinline__ void attn_issue_pv(AttnGeom& g, int t_lo, Resolve&& r
 
 // Epilogue of a softmax thread: its row of O from tensor memory, divided by l, to global memory as bf16 (and the
 // row's log-sum-exp when asked for).
-// MX: over a microscaled cache.  O is that of values times 2^-16, and v_nan has, per 32 columns, the first chunk position that sees
-// a value that is not finite (attn_mx_loader.cuh).
-template <bool MX>
-__device__ __forceinline__ float attn_inverse(float l) { return MX ? 65536.f / l : 1.f / l; }
-template <bool MX>
+// FMT: over a microscaled cache of that format (0: bf16).  O is that of values times 2^-16 and has its columns in the order of
+// mx_place, and v_nan has, per 32 columns, the first chunk position that sees a value that is not finite (attn_mx_loader.cuh).
+template <int FMT>
+__device__ __forceinline__ constexpr int mx_place(int e) {
+  return FMT == QUOKA_KV_MXFP8 ? (e & ~3) | (e & 1) << 1 | (e & 2) >> 1 : FMT == QUOKA_KV_MXFP4 ? (e & ~7) | (e & 3) << 1 | (e & 4) >> 2 : e;
+}
+template <int FMT>
+__device__ __forceinline__ float attn_inverse(float l) { return FMT != 0 ? 65536.f / l : 1.f / l; }
+template <int FMT>
 __device__ __forceinline__ void attn_mark_nan(uint32_t (&r)[32], const int* v_nan, int c, int row) {
-  if constexpr (MX) {
+  if constexpr (FMT != 0) {
     if (v_nan[c] <= row) {
 #pragma unroll
       for (int i = 0; i < 32; ++i) r[i] = 0x7FC00000u;
     }
   }
 }
-template <int D, bool MX = false>
+template <int D, int FMT = 0>
 __device__ __forceinline__ void attn_store_row(const DevParams& P, uint32_t o_addr, float m_run, float l_run, int s, int h,
                                                int row, bool store, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                                                const int* v_nan = nullptr) {
-  const float inv = attn_inverse<MX>(l_run);
+  const float inv = attn_inverse<FMT>(l_run);
   __nv_bfloat16* orow = out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)row * P.o_st;
 #pragma unroll
   for (int c = 0; c < D / 32; ++c) {
     uint32_t r[32];
     tmem_ld32(o_addr + c * 32, r);
     tmem_wait_ld();
-    attn_mark_nan<MX>(r, v_nan, c, row);
+    attn_mark_nan<FMT>(r, v_nan, c, row);
     if (store) {
 #pragma unroll
       for (int v4 = 0; v4 < 4; ++v4) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(r[v4 * 8 + 2 * i]) * inv,
-                                                           __uint_as_float(r[v4 * 8 + 2 * i + 1]) * inv);
+          const __nv_bfloat162 b2 = __floats2bfloat162_rn(__uint_as_float(r[mx_place<FMT>(v4 * 8 + 2 * i)]) * inv,
+                                                           __uint_as_float(r[mx_place<FMT>(v4 * 8 + 2 * i + 1)]) * inv);
           w[i] = *reinterpret_cast<const uint32_t*>(&b2);
         }
         *reinterpret_cast<uint4*>(orow + c * 32 + v4 * 8) = make_uint4(w[0], w[1], w[2], w[3]);
@@ -501,7 +505,7 @@ __device__ __forceinline__ void attn_store_row(const DevParams& P, uint32_t o_ad
 constexpr int kSplitTileFloats = 130 * 128;     // one part's partial result of a 128-row Q tile
 
 // Epilogue of a softmax warp of a split launch.
-template <int D, bool MX = false>
+template <int D, int FMT = 0>
 __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job, int part, int n_parts, int x, int quarter,
                                                     int lane, int row_in_tile, int row, bool store, bool have, uint32_t o_addr,
                                                     float m_run, float l_run, int s, int h, __nv_bfloat16* out,
@@ -519,9 +523,9 @@ __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job,
       uint32_t r[32];
       tmem_ld32(o_addr + c * 32, r);
       tmem_wait_ld();
-      attn_mark_nan<MX>(r, v_nan, c, row);
+      attn_mark_nan<FMT>(r, v_nan, c, row);
 #pragma unroll
-      for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row_in_tile] = __uint_as_float(r[i]);
+      for (int i = 0; i < 32; ++i) mine[(c * 32 + i) * 128 + row_in_tile] = __uint_as_float(r[mx_place<FMT>(i)]);
     }
   }
   mine[D * 128 + row_in_tile] = have ? m_run : -INFINITY;
@@ -549,7 +553,7 @@ __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job,
       if (q < n_parts) l += w * __ldcg(tile0 + (size_t)q * 2 * kTile + (D + 1) * 128 + row_in_tile);
       wgt[q] = w;
     }
-    const float inv = attn_inverse<MX>(l);
+    const float inv = attn_inverse<FMT>(l);
     __nv_bfloat16* orow = out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)row * P.o_st;
 #pragma unroll 1
     for (int c = 0; c < D / 32; ++c) {
@@ -588,7 +592,7 @@ __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job,
 constexpr int kPartPitch = 132;                  // floats per row: 16 bytes off a multiple of the banks
 
 // A softmax thread's row of O, its m and l.  Nothing of the CTA may still read the shared memory below `smem` + 2 tiles.
-template <int D, bool MX = false>
+template <int D, int FMT = 0>
 __device__ __forceinline__ void attn_part_to_smem(unsigned char* smem, float* ml, int x, int row_in_tile, bool have, uint32_t o_addr,
                                                   float m_run, float l_run, int chunk_row = 0, const int* v_nan = nullptr) {
   float* row = reinterpret_cast<float*>(smem) + (x * 128 + row_in_tile) * kPartPitch;
@@ -598,10 +602,11 @@ __device__ __forceinline__ void attn_part_to_smem(unsigned char* smem, float* ml
       uint32_t r[32];
       tmem_ld32(o_addr + c * 32, r);
       tmem_wait_ld();
-      attn_mark_nan<MX>(r, v_nan, c, chunk_row);
+      attn_mark_nan<FMT>(r, v_nan, c, chunk_row);
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        *reinterpret_cast<uint4*>(row + c * 32 + 4 * i) = make_uint4(r[4 * i], r[4 * i + 1], r[4 * i + 2], r[4 * i + 3]);
+        *reinterpret_cast<uint4*>(row + c * 32 + 4 * i) = make_uint4(r[mx_place<FMT>(4 * i)], r[mx_place<FMT>(4 * i + 1)],
+                                                                                 r[mx_place<FMT>(4 * i + 2)], r[mx_place<FMT>(4 * i + 3)]);
     }
   }
   ml[x * 256 + row_in_tile] = have ? m_run : -INFINITY;
@@ -612,7 +617,7 @@ __device__ __forceinline__ void attn_part_to_smem(unsigned char* smem, float* ml
 // elements per lane, in a loop kept small: this code runs once per launch, and instructions have to be fetched too (four rows
 // side by side per warp, 10 KB of code, took 7.3 us for 32 rows of a CTA and four parts; this form 4.8: the reads of other
 // CTAs' shared memory, 50 KB at about 14 bytes per clock).
-template <int D, bool MX = false>
+template <int D, int FMT = 0>
 __device__ __forceinline__ void attn_merge_cluster(const DevParams& P, unsigned char* smem, float* ml, int warp, int n_warps, int lane,
                                                    int stride, int offset, int parts, int part, const QRows& qr, int s,
                                                    __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
@@ -646,7 +651,7 @@ __device__ __forceinline__ void attn_merge_cluster(const DevParams& P, unsigned 
       acc.x = fmaf(w, o.x, acc.x); acc.y = fmaf(w, o.y, acc.y);
       acc.z = fmaf(w, o.z, acc.z); acc.w = fmaf(w, o.w, acc.w);
     }
-    const float inv = attn_inverse<MX>(L);
+    const float inv = attn_inverse<FMT>(L);
     const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), b = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
     const int h = qr.head(P, lr), p = qr.position(P, x, lr);
     *reinterpret_cast<uint2*>(out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)p * P.o_st + 4 * lane) =
