@@ -16,6 +16,8 @@
 // Arithmetic intensity is N flop per byte of K: HBM-bound below N ~ 200, tensor-bound above.
 #include <cstdio>
 
+#include "mx_host.cuh"
+#include "mx_rows.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_kernels.cuh"
 
@@ -25,6 +27,12 @@ using namespace ptx;
 
 constexpr int kTileKeys = 128;
 constexpr int kScoreThreads = 320;          // 10 warps: TMA, MMA, two epilogue groups of four
+// Over a microscaled cache four loader warps more, which bring the key rows in and convert them (mx_rows.cuh); warp 0 has Q-bar only.
+constexpr int kScoreLoaders = 4, kScoreMxThreads = kScoreThreads + 32 * kScoreLoaders;
+template <int FMT, int D>
+using ScoreRows = MxItem<FMT, D, 128, D, kScoreLoaders, /*PLAIN=*/true>;
+template <int FMT, int D>
+constexpr uint32_t kScoreWarpStage = ScoreRows<FMT, D>::kRaw + (D == 128 ? 128 : 256);
 constexpr uint32_t kTmemCols = 512;
 constexpr int kMaxStages = 8;
 
@@ -37,7 +45,7 @@ struct ScoreSmemPlan {
   size_t q_bytes, stage_bytes, total;
 };
 
-static ScoreSmemPlan plan_score_smem(int N, int d) {
+static ScoreSmemPlan plan_score_smem(int N, int d, size_t raw = 0) {
   ScoreSmemPlan pl{};
   pl.n_pad = (N + 15) / 16 * 16;
   pl.n_parts = pl.n_pad > 256 ? 2 : 1;
@@ -45,10 +53,10 @@ static ScoreSmemPlan plan_score_smem(int N, int d) {
   pl.q_rows = pl.n_parts * pl.box_rows;
   pl.q_bytes = (size_t)pl.q_rows * d * 2;
   pl.stage_bytes = (size_t)kTileKeys * d * 2;
-  const size_t budget = 227 * 1024 - 2048;    // alignment slack + barriers
-  int st = (int)((budget - pl.q_bytes) / pl.stage_bytes);
+  const size_t budget = 227 * 1024 - 2048 - raw;    // alignment slack + barriers; raw rows of a microscaled cache
+  int st = budget > pl.q_bytes ? (int)((budget - pl.q_bytes) / pl.stage_bytes) : 0;
   pl.stages = st > kMaxStages ? kMaxStages : st;
-  pl.total = 1024 + pl.q_bytes + pl.stages * pl.stage_bytes + 1024;
+  pl.total = 1024 + pl.q_bytes + pl.stages * pl.stage_bytes + 1024 + raw;
   return pl;
 }
 
@@ -92,10 +100,12 @@ __device__ __forceinline__ long long total_tiles(const DevParams& P) {
   return t;
 }
 
-template <int HALVES>   // head_dim / 64
-__global__ void __launch_bounds__(kScoreThreads, 1)
+// head_dim / 64; format of the cache (0: bf16, tm_k), of a microscaled one (k) the items of raw rows on their way
+template <int HALVES, int FMT = 0, int NST = 0>
+__global__ void __launch_bounds__(FMT != 0 ? kScoreMxThreads : kScoreThreads, 1)
 score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorMap tm_q,
-                     const __grid_constant__ CUtensorMap tm_k, float* __restrict__ scores) {
+                     const __grid_constant__ CUtensorMap tm_k, const void* __restrict__ k, float* __restrict__ scores) {
+  constexpr bool MX = FMT != 0;
   constexpr uint32_t kHalfBytes = kTileKeys * 128;             // one 64-column half of a K tile
   constexpr uint32_t kStageBytes = HALVES * kHalfBytes;
   extern __shared__ unsigned char smem_raw[];
@@ -118,13 +128,13 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
 
   if (threadIdx.x == 0) {
     abort_flag = 0;
-    for (int i = 0; i < A.stages; ++i) { mbar_init(&full[i], 1); mbar_init(&empty[i], 5); }
+    for (int i = 0; i < A.stages; ++i) { mbar_init(&full[i], MX ? kScoreLoaders : 1); mbar_init(&empty[i], 5); }
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
-    tma_prefetch_desc(&tm_k);
+    if (!MX) tma_prefetch_desc(&tm_k);
   }
   if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
   tc_fence_before();
@@ -158,6 +168,16 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
             tma_load_3d(q_smem + (size_t)h * q_half_bytes + (size_t)p * A.box_rows * 128, &tm_q, q_full, h * 64,
                         p * A.box_rows, head);
       };
+      if constexpr (MX) {                             // Q-bar alone
+        for (; w.valid(); w.next(P)) {
+          const int head = w.s * P.n_kv + w.kv;
+          if (head == head_cur) continue;
+          if (head_cur >= 0) { if (!mbar_wait(q_empty, qe_phase, wc)) break; qe_phase ^= 1; }
+          load_q(head);
+          head_cur = head;
+        }
+        if (!waited) grid_dependency_wait();
+      } else {
       for (; w.valid(); w.next(P)) {
         const int head = w.s * P.n_kv + w.kv;
         if (head != head_cur) {
@@ -189,6 +209,47 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
       if (q_deferred >= 0) load_q(q_deferred);
       // a CTA without tiles still waits: the chain of a fused call is only transitive if every link has waited
       if (!waited) grid_dependency_wait();
+      }
+    }
+  } else if (MX && warp >= kScoreThreads / 32) {
+    // ------------------------------------------------------------------ microscaled cache: key rows in, converted
+    if constexpr (MX) {
+      typedef ScoreRows<FMT, 64 * HALVES> Rows;
+      constexpr uint32_t kWarpStage = kScoreWarpStage<FMT, 64 * HALVES>;
+      const int lw = warp - kScoreThreads / 32, my_row = Rows::row(lw, lane);
+      const uint32_t stage0 = smem_u32(reinterpret_cast<unsigned char*>(bars) + 1024) + (uint32_t)lw * (NST * kWarpStage);
+      MxPlaces places(P);
+      TileWalk in; in.seek(P, lo, hi);
+      TileWalk w = in;
+      const auto copy = [&](int at) {                 // the next tile's rows (keys past the sequence are zeros, their scores are not written)
+        if (in.valid()) {
+          const int t = in.tile * kTileKeys + my_row;
+          uint32_t place, srow;
+          places.at_head(P, in.s, in.kv);
+          places.of(P, t < __ldg(P.ctx_len + in.s) ? t : -1, place, srow);
+          const uint32_t raw = stage0 + (uint32_t)at * kWarpStage;
+          Rows::copy(static_cast<const typename Rows::W*>(k), place, P.k_scale, srow, raw, raw + Rows::kRaw, lane);
+          in.next(P);
+        }
+        cp_async_commit();
+      };
+#pragma unroll
+      for (int i = 0; i < NST; ++i) copy(i);
+      int stage = 0, at = 0; uint32_t phase = 0;
+      for (; w.valid(); w.next(P)) {
+        cp_async_wait<NST - 1>();
+        __syncwarp();
+        if (!mbar_wait(&empty[stage], phase ^ 1, wc)) break;
+        const uint32_t raw = stage0 + (uint32_t)at * kWarpStage;
+        Rows::convert(raw, Rows::scales(raw + Rows::kRaw, lane), 0, kBf16Nan2, k_smem + (size_t)stage * kStageBytes, lw, lane);
+        fence_proxy_async_smem();                     // these stores, before products read the stage
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&full[stage]);
+        copy(at);
+        if (++at == NST) at = 0;
+        if (++stage == A.stages) { stage = 0; phase ^= 1; }
+      }
+      cp_async_wait_all();
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (the whole warp, one lane issues)
@@ -256,6 +317,7 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
       const int T_s = __ldg(P.ctx_len + w.s);
       const int t = w.tile * kTileKeys + row;
       const bool own_norm = P.k_inv_norm == nullptr && !P.score_dot;
+      constexpr float kUnshift = MX ? kMxUnshift : 1.f;     // (the tile's values are the cache's times 2^-16)
       float inv_cached = 1.f;
       if (P.k_inv_norm != nullptr && !P.score_dot)
         inv_cached = __ldg(P.k_inv_norm + kv_norm_index(P, w.s, w.kv, min(t, T_s - 1)));
@@ -346,7 +408,7 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
       if (lane == 0) mbar_arrive(&acc_empty[slot]);
       if (t < T_s)
         scores[((long long)w.s * P.n_kv + w.kv) * P.max_ctx + t] =
-            own_norm ? best / fmaxf(sqrtf(nn), kNormEps) : best * inv_cached;
+            own_norm ? best / fmaxf(sqrtf(nn), kNormEps / kUnshift) : best * kUnshift * inv_cached;
       if (++stage == A.stages) { stage = 0; phase ^= 1; }
     }
   }
@@ -401,6 +463,16 @@ bool score_keys_tc_supported(const quoka_params* p) {
   return true;
 }
 
+template <typename Kernel>
+static cudaError_t launch_score(Kernel kernel, const char* name, int grid, int threads, size_t smem, cudaStream_t st, bool chained, const DevParams& P,
+                                const ScoreArgs& A, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const void* k, float* scores) {
+  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  e = launch_kernel(name, kernel, dim3(grid), dim3(threads), smem, st, 1, chained, P, A, tm_q, tm_k, k, scores);
+  if (e == cudaSuccess) count_launch();
+  return e;
+}
+
 quoka_status launch_score_keys_tc(const quoka_params* p, const DevParams& P, const void* qbar, const void* k,
                                   float* scores, cudaStream_t st, bool chained) {
   const int N = P.n_sel;
@@ -420,17 +492,38 @@ quoka_status launch_score_keys_tc(const quoka_params* p, const DevParams& P, con
   if (grid <= 0) return QUOKA_ERR_CUDA;
   if (max_tiles < grid) grid = (int)max_tiles;
   if (grid <= 0) return QUOKA_OK;
-  cudaError_t e;
-  if (P.d == 128) {
-    e = cudaFuncSetAttribute(score_keys_tc_kernel<2>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.total);
-    if (e != cudaSuccess) return QUOKA_ERR_CUDA;
-    e = launch_kernel("score_keys_tc", score_keys_tc_kernel<2>, dim3(grid), dim3(kScoreThreads), pl.total, st, 1, chained, P, A, tm_q, tm_k, scores);
-  } else {
-    e = cudaFuncSetAttribute(score_keys_tc_kernel<1>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)pl.total);
-    if (e != cudaSuccess) return QUOKA_ERR_CUDA;
-    e = launch_kernel("score_keys_tc", score_keys_tc_kernel<1>, dim3(grid), dim3(kScoreThreads), pl.total, st, 1, chained, P, A, tm_q, tm_k, scores);
-  }
-  count_launch();
+  const cudaError_t e = launch_score(P.d == 128 ? score_keys_tc_kernel<2> : score_keys_tc_kernel<1>, "score_keys_tc", grid, kScoreThreads, pl.total, st, chained, P,
+                                     A, tm_q, tm_k, nullptr, scores);
+  return (e == cudaSuccess && cudaGetLastError() == cudaSuccess) ? QUOKA_OK : QUOKA_ERR_CUDA;
+}
+
+bool score_keys_mx_tc_supported(const quoka_params* p) { return score_keys_tc_supported(p) && attn_mx_tc_supported(p); }
+
+quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st,
+                                     bool chained) {
+  const int N = P.n_sel;
+  // Three items of raw rows on their way, one where the retained queries (more than 256 at head_dim 128) leave no room for them.
+  const size_t item = kScoreLoaders * (P.d == 128 ? (fmt == QUOKA_KV_MXFP8 ? kScoreWarpStage<QUOKA_KV_MXFP8, 128> : kScoreWarpStage<QUOKA_KV_MXFP4, 128>)
+                                                  : (fmt == QUOKA_KV_MXFP8 ? kScoreWarpStage<QUOKA_KV_MXFP8, 64> : kScoreWarpStage<QUOKA_KV_MXFP4, 64>));
+  const bool three = plan_score_smem(N, P.d, 3 * item).stages >= 3;
+  const ScoreSmemPlan pl = plan_score_smem(N, P.d, (three ? 3 : 1) * item);
+  if (pl.stages < 2) return QUOKA_ERR_UNSUPPORTED;
+  CUtensorMap tm_q, none = {};
+  const uint64_t dims[3] = {(uint64_t)P.d, (uint64_t)N, (uint64_t)P.batch * P.n_kv};
+  const uint64_t strides[2] = {(uint64_t)P.d * 2, (uint64_t)N * P.d * 2};
+  const uint32_t box[3] = {64, (uint32_t)pl.box_rows, 1};
+  if (!encode_tensor_map_bf16(&tm_q, qbar, 3, dims, strides, box)) return QUOKA_ERR_CUDA;
+  ScoreArgs A{N, pl.n_pad, pl.n_parts, pl.box_rows, pl.q_rows, pl.stages, 0};
+  const long long max_tiles = (long long)P.batch * P.n_kv * ((P.max_ctx + kTileKeys - 1) / kTileKeys);
+  int grid = device_sm_count();
+  if (grid <= 0) return QUOKA_ERR_CUDA;
+  if (max_tiles < grid) grid = (int)max_tiles;
+  if (grid <= 0) return QUOKA_OK;
+  const cudaError_t e = mx_dispatch(QUOKA_BF16, fmt, P.d, [&](auto, auto f, auto d) {
+    constexpr int FMT = decltype(f)::value, H = decltype(d)::value / 64;
+    return launch_score(three ? score_keys_tc_kernel<H, FMT, 3> : score_keys_tc_kernel<H, FMT, 1>, "score_keys_mx_tc", grid, kScoreMxThreads, pl.total, st, chained,
+                        P, A, tm_q, none, k, scores);
+  });
   return (e == cudaSuccess && cudaGetLastError() == cudaSuccess) ? QUOKA_OK : QUOKA_ERR_CUDA;
 }
 

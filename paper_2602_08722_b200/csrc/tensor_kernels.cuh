@@ -40,6 +40,9 @@ quoka_status launch_attn_tc_pair(const quoka_params* p, const DevParams& P, cons
                                  bool after_selection, const AttnPlan& plan);
 
 // The same over a microscaled cache (the scale arrays in P).
+bool score_keys_mx_tc_supported(const quoka_params* p);
+quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st,
+                                     bool chained);
 bool attn_mx_tc_supported(const quoka_params* p);
 quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* q, const void* k, const void* v,
                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, bool after_selection,
