@@ -31,12 +31,14 @@ namespace quoka {
 
 template <int D, int FMT = 0>
 constexpr int kSlotsOf = D == 64 ? 8 : FMT == 0 ? 5 : 4;     // of 16 KB, 32 KB
+template <int D, int FMT>
+constexpr int kMxStagesOf = D == 64 ? 4 : FMT == QUOKA_KV_MXFP8 ? 2 : 3;      // raw items of 16 KB beside four slots, or smaller ones
 template <int D, int FMT, bool SPARSE>
-using MxTileLoader = MxLoader<FMT, D, 128, D, SPARSE, kMxLoaderWarps, kSlotsOf<D, FMT>, D == 128 && FMT == QUOKA_KV_MXFP8 ? 2 : 3>;
+using MxTileLoader = MxLoader<FMT, D, 128, D, SPARSE, kSlotsOf<D, FMT>, kMxStagesOf<D, FMT>>;
 template <int D, int FMT = 0>
 constexpr size_t attn_tc_smem() {
   size_t n = 1024 + (size_t)(2 + kSlotsOf<D, FMT>) * (D / 64) * 16384 + 512;
-  if constexpr (FMT != 0) n += MxTileLoader<D, FMT, false>::kStageBytes;
+  if constexpr (FMT != 0) n += MxTileLoader<D, FMT, false>::kBytes;
   return n;
 }
 
@@ -67,7 +69,9 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
   uint64_t* o_full = p_done + NBUF;         // [2]       MMA commit after the last PV
   uint64_t* q_full = o_full + 2;            // TMA
   uint64_t* q_ready = q_full + 1;           // MX: the Q tiles are in the order of the converted rows, 4 loader warps
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 1);
+  uint64_t* raw_full = q_ready + 1;         // MX: [2][kMxStages] raw items, full and empty
+  constexpr int kMxStages = kMxStagesOf<D, FMT>;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(raw_full + 2 * kMxStages);
   __shared__ int abort_flag;
   __shared__ int v_nan[D / kMxBlock];       // MX
 
@@ -101,14 +105,14 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     for (int i = 0; i < 2; ++i) mbar_init(&o_full[i], 1);
     mbar_init(q_full, 1);
     mbar_init(q_ready, kMxLoaderWarps);
-    fence_mbar_init();
     tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
     if constexpr (MX) {
       for (int i = 0; i < D / kMxBlock; ++i) v_nan[i] = kNoNan;
-    } else {
-      tma_prefetch_desc(&tm_k);
-      tma_prefetch_desc(&tm_v);
+      for (int i = 0; i < kMxStages; ++i) { mbar_init(&raw_full[i], kMxCopyWarps * 33); mbar_init(&raw_full[kMxStages + i], kMxLoaderWarps); }
     }
+    fence_mbar_init();
   }
   if (warp == kQkWarp) tmem_alloc(tmem_slot, 512);
   zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
@@ -176,15 +180,20 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
                              row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s, qr.head(P, row_in_tile),
                              out, lse, v_nan);
     }
-  } else if (MX ? warp >= kMxFirstLoader : warp < 8 + kLoaderWarps) {
+  } else if (MX && warp >= kMxFirstLoader) {
+    // ================================================================== microscaled cache: rows converted
+    if constexpr (MX) {
+      MxTileLoader<D, FMT, SPARSE> loader{P, s, kv, lane, 0, 0, reinterpret_cast<unsigned char*>(bars) + 512, raw_full, raw_full + kMxStages};
+      if (mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc))
+        loader.convert(g, t_lo, warp - kMxFirstLoader, kv_smem, kTileBytes, kv_full, kv_empty, v_nan, wc, [&]() { resolve(g, k_cnt, s); });
+    }
+  } else if (warp < 8 + kLoaderWarps) {
     // ================================================================== K / V row loaders (gather)
     // One warp instruction copies four whole rows (eight lanes x 16 bytes cover a 128-byte row; head_dim 128: two); the row
     // groups of a tile are dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxTileLoader<D, FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 0, 0, g.T, kc, vc, k_idx, v_nan, reinterpret_cast<unsigned char*>(bars) + 512);
-      loader.run(g, t_lo, kv_smem, kTileBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); }, [&]() {
-        return mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc);
-      });
+      MxTileLoader<D, FMT, SPARSE> loader{P, s, kv, lane, 0, 0, reinterpret_cast<unsigned char*>(bars) + 512, raw_full, raw_full + kMxStages};
+      loader.fill(g, t_lo, warp - 8, kc, vc, k_idx, &tm_k, &tm_v, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;
     constexpr int PIECES = D / 8;                             // 16-byte pieces per row (16 or 8)
@@ -306,7 +315,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     cp_async_wait_all();                                      // nothing of this thread is in flight at exit
     }
-  } else if (!MX || warp >= kPvWarp) {
+  } else {
     // ================================================================== warp 11: QK^T, warp 10: PV
     if (warp == kQkWarp && lane == 0) load_q_tiles<D>(P, qr, q_smem, &tm_q, q_full, s);
     __syncwarp();

@@ -25,8 +25,10 @@ quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P0, int f
                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, bool after_selection,
                                const AttnPlan& plan) {
   const DevParams P = attn_of_plan(P0, plan);
-  CUtensorMap tm_q, none = {};
+  CUtensorMap tm_q, tm_k, tm_v;
   if (!encode_q_tensor_map(&tm_q, P, q)) return QUOKA_ERR_CUDA;
+  // (a pair's CTA takes half of V's columns)
+  if (!encode_mx_tensor_map(&tm_k, p, fmt, k, P.d) || !encode_mx_tensor_map(&tm_v, p, fmt, v, plan.ctas == 2 ? 64 : P.d)) return QUOKA_ERR_CUDA;
   const bool pair = plan.ctas == 2, wide = P.d == 128, fp8 = fmt == QUOKA_KV_MXFP8;
   AttnKernel (*const kernel)(bool, bool, bool) = pair ? (fp8 ? pick<true, true, true> : pick<true, true, false>)
                                                  : wide ? (fp8 ? pick<false, true, true> : pick<false, true, false>)
@@ -35,7 +37,7 @@ quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P0, int f
                       : wide ? (fp8 ? attn_tc_smem<128, QUOKA_KV_MXFP8>() : attn_tc_smem<128, QUOKA_KV_MXFP4>())
                              : (fp8 ? attn_tc_smem<64, QUOKA_KV_MXFP8>() : attn_tc_smem<64, QUOKA_KV_MXFP4>());
   return launch_attn_plan(p, P, plan, kernel, pair ? "attn_tc_pair_mx" : "attn_tc_mx", pair ? 2 : 1, kMxAttnThreads,
-                          smem, tm_q, none, none, k, v, k_idx, k_cnt, out, lse, st,
+                          smem, tm_q, tm_k, tm_v, k, v, k_idx, k_cnt, out, lse, st,
                           after_selection);
 }
 

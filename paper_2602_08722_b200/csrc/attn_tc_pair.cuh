@@ -37,7 +37,7 @@ constexpr uint32_t kPairSlotBytes = 16384;
 constexpr uint32_t kPairQTileBytes = 32768;
 
 template <int FMT, bool SPARSE>
-using MxPairLoader = MxLoader<FMT, 128, 64, 64, SPARSE, kMxLoaderWarps, kPairSlots, 3>;
+using MxPairLoader = MxLoader<FMT, 128, 64, 64, SPARSE, kPairSlots, 3>;
 
 enum { kWhole = 0, kParts = 1, kPartsCluster = 2 };     // a row block per pair; parts merged through memory / in a cluster
 
@@ -68,7 +68,9 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
   uint64_t* q_full = o_full + 2;                  // this CTA's Q tiles (TMA)
   uint64_t* peer_q = q_full + 1;                  // first CTA only: the second CTA's Q tiles have landed
   uint64_t* q_ready = peer_q + 1;                 // MX: this CTA's Q tiles are in the order of the converted rows, 4 loader warps
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_ready + 1);
+  uint64_t* raw_full = q_ready + 1;               // MX: [2][kMxStages] raw items, full and empty
+  constexpr int kMxStages = 3;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(raw_full + 2 * kMxStages);
   float* part_ml = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);   // [2][m | l][128], kPartsCluster
   __shared__ int abort_flag;
   __shared__ int v_nan[D / kMxBlock];             // MX
@@ -100,14 +102,14 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     mbar_init(q_full, 1);
     mbar_init(peer_q, 1);
     mbar_init(q_ready, kMxLoaderWarps);
-    fence_mbar_init();
     tma_prefetch_desc(&tm_q);
+    tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_v);
     if constexpr (MX) {
       for (int i = 0; i < D / kMxBlock; ++i) v_nan[i] = kNoNan;
-    } else {
-      tma_prefetch_desc(&tm_k);
-      tma_prefetch_desc(&tm_v);
+      for (int i = 0; i < kMxStages; ++i) { mbar_init(&raw_full[i], kMxCopyWarps * 33); mbar_init(&raw_full[kMxStages + i], kMxLoaderWarps); }
     }
+    fence_mbar_init();
   }
   if (warp == kQkWarp) tmem_alloc_pair(tmem_slot, 512);
   zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
@@ -192,17 +194,23 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
                              quarter, lane, row_in_tile, row, row_in_tile < qr.count(P, x), have, o_addr, m_run, l_run, s,
                              qr.head(P, row_in_tile), out, lse, v_nan);
     }
-  } else if (MX ? warp >= kMxFirstLoader : warp < 8 + kPairLoaderWarps) {
+  } else if (MX && warp >= kMxFirstLoader) {
+    // ================================================================== microscaled cache: rows converted
+    if constexpr (MX) {
+      MxPairLoader<FMT, SPARSE> loader{P, s, kv, lane, 64 * (int)rank, 64 * (int)rank, reinterpret_cast<unsigned char*>(bars) + 512 + (MODE == kPartsCluster ? 2048 : 0), raw_full,
+                                     raw_full + kMxStages};
+      if (mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kPairQTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc))
+        loader.convert(g, t_lo, warp - kMxFirstLoader, kv_smem, kPairSlotBytes, kv_full, kv_empty, v_nan, wc, [&]() { resolve(g, k_cnt, s); });
+    }
+  } else if (warp < 8 + kPairLoaderWarps) {
     // ================================================================== K / V loaders: this CTA's half of every tile
     // K item: tile rows [64 * rank, 64 * rank + 64), 256 bytes each (16 pieces, 2 rows per warp instruction).
     // V item: all 128 tile rows, bytes [128 * rank, 128 * rank + 128) of each (8 pieces, 4 rows per instruction).
     // Either way an item is 32 row groups, dealt round-robin to the loader warps.
     if constexpr (MX) {
-      MxPairLoader<FMT, SPARSE> loader(P, s, kv, warp - kMxFirstLoader, lane, 64 * (int)rank, 64 * (int)rank, g.T, kc, vc, k_idx, v_nan,
-                                       reinterpret_cast<unsigned char*>(bars) + 512 + (MODE == kPartsCluster ? 2048 : 0));
-      loader.run(g, t_lo, kv_smem, kPairSlotBytes, kv_full, kv_empty, wc, [&]() { resolve(g, k_cnt, s); }, [&]() {
-        return mx_order_q<FMT>(q_smem, P.attn_qtiles * (int)kPairQTileBytes, threadIdx.x - 32 * kMxFirstLoader, 32 * kMxLoaderWarps, q_full, q_ready, wc);
-      });
+      MxPairLoader<FMT, SPARSE> loader{P, s, kv, lane, 64 * (int)rank, 64 * (int)rank, reinterpret_cast<unsigned char*>(bars) + 512 + (MODE == kPartsCluster ? 2048 : 0), raw_full,
+                                     raw_full + kMxStages};
+      loader.fill(g, t_lo, warp - 8, kc, vc, k_idx, &tm_k, &tm_v, wc, [&]() { resolve(g, k_cnt, s); });
     } else {
     const int lw = warp - 8;
     constexpr int GROUPS = 32;
@@ -312,8 +320,6 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     }
     cp_async_wait_all();                                      // nothing of this thread is in flight at exit
     }
-  } else if (MX && warp < kPvWarp) {
-    // (no role)
   } else if (rank != 0) {
     // ================================================================== second CTA, one thread of warps 10 and 11: forward
     // the "full" of the V (10) and K (11) slots to the first CTA
@@ -443,7 +449,7 @@ AttnKernel pick_attn_tc_pair(bool sparse, bool parts, bool in_cluster) {
 template <int FMT>
 size_t attn_tc_pair_smem(const AttnPlan& plan) {
   size_t n = 1024 + 2 * kPairQTileBytes + (size_t)kPairSlots * kPairSlotBytes + 512 + (plan.in_cluster ? 2048 : 0);
-  if constexpr (FMT != 0) n += MxPairLoader<FMT, false>::kStageBytes;
+  if constexpr (FMT != 0) n += MxPairLoader<FMT, false>::kBytes;
   return n;
 }
 

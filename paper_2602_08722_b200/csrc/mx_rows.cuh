@@ -5,6 +5,8 @@
 // factor a bf16 number for every e that a cache has.  All of it is exact; who uses the tile takes 2^-16 back.
 #pragma once
 
+#include <type_traits>
+
 #include "attn_tiles.cuh"
 #include "mx.cuh"
 
@@ -64,37 +66,36 @@ __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
-// One of NLW warps that bring items of cache rows into shared memory as bf16: of the ROWS tile rows from row0 on, or 128, the columns from
-// col0 on.  An item is [64-column halves][rows][128 B], 16-byte pieces swizzled by row.
-// The raw elements come in with cp.async, some items ahead of their conversion, into stages whose every piece is read by the
-// lane that copied it (8 or 16 bytes: a unit of 16 elements); a row's scale bytes by the lane that looks after the row.
-template <int FMT, int D, int ROWS, int COLS, int NLW, bool PLAIN>
+// An item is ROWS cache rows, COLS columns of each: raw in a stage of shared memory, [ROWS][COLS * bits / 8 bytes] and a word of
+// scale bytes per row, then bf16 in a tile, [64-column halves][ROWS][128 B] with 16-byte pieces swizzled by row.  What fills stages (the
+// copy engine where rows follow one another, else cp.async) and what converts them are different warps: each of the two alone, one
+// after the other in the same warps, took longer than a step of the attention kernel.
+template <int FMT, int D, int ROWS, int COLS>
 struct MxItem {
-  static constexpr int U = COLS / 16;                                  // units per row
+  static constexpr int U = COLS / 16;                                  // units of 16 elements per row
   static constexpr int RPI = 32 / U;                                   // rows per warp instruction
-  static constexpr int GROUPS = ROWS / (RPI * NLW);                    // row groups of this warp
-  static constexpr int kRows = GROUPS * RPI;                           // its rows, a lane each
-  static constexpr int kUnitBytes = 2 * kMxBits<FMT>;
-  static constexpr uint32_t kRaw = GROUPS * 32 * kUnitBytes;           // of a stage: this warp's units
+  static constexpr int kRows = ROWS, kHalves = U / 4;
+  static_assert(U == 8 || U == 4, "64 or 128 columns");
+  static constexpr int kUnitBytes = 2 * kMxBits<FMT>, kRowBytes = U * kUnitBytes;
+  static constexpr uint32_t kRaw = ROWS * kRowBytes, kStage = kRaw + ROWS * 4;     // of a stage
   static constexpr uint32_t kHalf = ROWS * 128;
-  static_assert(kRows <= 32 && GROUPS >= 1 && GROUPS * RPI * NLW == ROWS, "a lane per row");
   typedef decltype(MxUnit<FMT>::w) W;
 
-  // this lane's row of the item
-  static __device__ __forceinline__ int row(int lw, int lane) { return (lw + lane / RPI * NLW) * RPI + lane % RPI; }
-
-  // The copies of one item: `place` is this lane's row in units of 16 elements from `base` (kNoRow: zeros), `srow` its index among the
-  // rows of scales; raw: shared memory of this warp's units; meta: 32 scale words, head_dim 64 also 32 shifts.
-  static __device__ __forceinline__ void copy(const W* base, uint32_t place, const uint8_t* scale, uint32_t srow, uint32_t raw, uint32_t meta, int lane) {
-    if (place != kNoRow)                              // (head_dim 64: the word that has the scales of two rows)
-      cp_async_4(meta + 4 * lane, scale + (D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4));
-    else
-      asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 4 * lane), "r"(0u) : "memory");
-    if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 128 + 4 * lane), "r"((srow & 1u) * 16) : "memory");
+  // ---- filling, one of NW warps: lane l looks after rows row(0, l), row(1, l) ..
+  template <int NW> static constexpr int kMine = (ROWS / NW + 31) / 32;      // (1 or 2)
+  template <int NW> static __device__ __forceinline__ int row(int w, int i, int lane) {
+    const int p = 32 * i + lane;
+    return p < ROWS / NW ? (w + p / RPI * NW) * RPI + p % RPI : ROWS;
+  }
+  // this lane's copies: its pieces of the warp's rows, whose places (in units from `base`, kNoRow: zeros) the lanes that look after them have
+  template <int NW>
+  static __device__ __forceinline__ void copy(const W* base, const uint32_t (&place)[kMine<NW>], uint32_t stage, int w, int lane) {
     base += lane % U;
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      const uint32_t at = __shfl_sync(0xFFFFFFFFu, place, i * RPI + lane / U), dst = raw + (uint32_t)(i * 32 + lane) * kUnitBytes;
+#pragma unroll 2                                     // (as for the conversion: few instructions)
+    for (int i = 0; i < ROWS / (RPI * NW); ++i) {
+      const int p = i * RPI + lane / U;
+      const uint32_t at = __shfl_sync(0xFFFFFFFFu, kMine<NW> == 1 || i * RPI < 32 ? place[0] : place[kMine<NW> - 1], p & 31);
+      const uint32_t dst = stage + (uint32_t)((w + i * NW) * RPI * kRowBytes + lane * kUnitBytes);
       const W* src = base + (at == kNoRow ? 0u : at);
       if constexpr (kUnitBytes == 16) {
         cp_async_16(dst, src, at != kNoRow);
@@ -104,50 +105,68 @@ struct MxItem {
       }
     }
   }
-  // the scale bytes of this lane's row, landed
-  static __device__ __forceinline__ uint32_t scales(uint32_t meta, int lane) {
-    uint32_t w;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(meta + 4 * lane) : "memory");
-    if (D == 64) {
-      uint32_t shift;
-      asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 128 + 4 * lane) : "memory");
-      w = w >> shift & 0xFFFFu;
-    }
-    return w;
+  // a row's scale bytes, and their word of the stage
+  static __device__ __forceinline__ uint32_t load_scales(const uint8_t* scale, uint32_t srow) {
+    return D == 128 ? __ldg(reinterpret_cast<const uint32_t*>(scale) + srow) : __ldg(reinterpret_cast<const uint16_t*>(scale) + srow);
   }
-  // The item as bf16; `mine`: scales(), block0: the item's first block of a row; blocks that are not finite become `nan2`.
-  static __device__ __forceinline__ void convert(uint32_t raw_at, uint32_t mine, int block0, uint32_t nan2, unsigned char* item, int lw, int lane) {
-    const int u = lane % U, rsub = lane / U;
-    const int sw = U == 8 ? u >> 2 : 0;               // lanes of the second half store their second piece first: other banks
-    W raw[GROUPS];
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      const uint32_t at = raw_at + (uint32_t)(i * 32 + lane) * kUnitBytes;
-      if constexpr (FMT == QUOKA_KV_MXFP8)
-        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw[i].x), "=r"(raw[i].y), "=r"(raw[i].z), "=r"(raw[i].w) : "r"(at) : "memory");
-      else
-        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(raw[i].x), "=r"(raw[i].y) : "r"(at) : "memory");
-    }
-#pragma unroll
-    for (int i = 0; i < GROUPS; ++i) {
-      const uint32_t b = __shfl_sync(0xFFFFFFFFu, mine, i * RPI + rsub) >> (8 * (block0 + (u >> 1))) & 0xFFu;
-      const uint32_t f = b == kMxNanScale ? nan2 : mx_factor2<FMT>(b);
-      const int r = (lw + i * NLW) * RPI + rsub;
-      unsigned char* dst = item + (uint32_t)(u >> 2) * kHalf + (uint32_t)r * 128u;
-      const uint32_t p0 = (uint32_t)(((2 * (u & 3) + sw) ^ r) & 7) << 4;
-      uint4 first, second;
-      if constexpr (FMT == QUOKA_KV_MXFP8) {
-        first = mx_to_bf16x8<FMT, PLAIN>(sw ? raw[i].z : raw[i].x, sw ? raw[i].w : raw[i].y, f);
-        second = mx_to_bf16x8<FMT, PLAIN>(sw ? raw[i].x : raw[i].z, sw ? raw[i].y : raw[i].w, f);
-      } else {
-        first = mx_to_bf16x8<FMT, PLAIN>(sw ? raw[i].y : raw[i].x, 0u, f);
-        second = mx_to_bf16x8<FMT, PLAIN>(sw ? raw[i].x : raw[i].y, 0u, f);
-      }
-      *reinterpret_cast<uint4*>(dst + p0) = first;
-      *reinterpret_cast<uint4*>(dst + (p0 ^ 16u)) = second;
-    }
+  static __device__ __forceinline__ void put_scales(uint32_t stage, int row, uint32_t word) {
+    asm volatile("st.shared.u32 [%0], %1;" ::"r"(stage + kRaw + 4 * row), "r"(word) : "memory");
   }
 };
+
+// Converting, one of NW warps: an item of `rows` rows of 64 or 128 columns (halves 1, 2) at row_bytes a row, in half tiles of half_bytes;
+// scales: the item's first scale byte of its first row; blocks that are not finite become `nan2`.  A warp instruction takes 64 columns of
+// eight rows, of the odd ones the other half: no two lanes of a quarter then meet in a bank, neither reading nor writing.
+// A loop, one step ahead with its loads, and the same few instructions for every kind of item: unrolled per kind they had to be
+// fetched anew for every item, beside those of the softmax (2048 queries of 32 heads over 16384 rows 610 us, 501 as a loop).
+template <int FMT, int NW, bool PLAIN>
+__device__ __forceinline__ void mx_convert(uint32_t stage, uint32_t scales, int rows, int halves, int row_bytes, uint32_t nan2, unsigned char* tile,
+                                           uint32_t half_bytes, int w, int lane) {
+  constexpr int kUnitBytes = 2 * kMxBits<FMT>;
+  typename std::remove_const<decltype(MxUnit<FMT>::w)>::type raw;
+  uint32_t b;
+  const int sub = lane >> 2, u = lane & 3, odd = sub & 1;
+  uint32_t src = stage + (uint32_t)((8 * w + sub) * row_bytes + u * kUnitBytes), sc = scales + (uint32_t)(4 * (8 * w + sub) + (u >> 1));
+  unsigned char* dst = tile + (uint32_t)(8 * w + sub) * 128u + ((uint32_t)(2 * u ^ sub) << 4);
+  const uint32_t second = (sub & 1) ? (uint32_t)-16 : 16u;     // the unit's other piece: 2 u + 1, swizzled
+  int steps = rows / (8 * NW) * halves, h = halves == 2 ? odd : 0;
+  const auto fetch = [&](int half) {
+    asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b) : "r"(sc + 2 * half) : "memory");
+    const uint32_t at = src + (uint32_t)(half * 4 * kUnitBytes);
+    if constexpr (FMT == QUOKA_KV_MXFP8)
+      asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(raw.x), "=r"(raw.y), "=r"(raw.z), "=r"(raw.w) : "r"(at) : "memory");
+    else
+      asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(raw.x), "=r"(raw.y) : "r"(at) : "memory");
+  };
+  fetch(h);
+#pragma unroll 1
+  for (;;) {
+    const auto now = raw;
+    const uint32_t f = b == kMxNanScale ? nan2 : mx_factor2<FMT>(b);
+    unsigned char* to = dst + (h ? half_bytes : 0u);
+    // the next step: the other half of these rows, or the next eight rows of this warp
+    if (halves == 2) h ^= 1;
+    if (halves == 1 || h == odd) {
+      src += 8 * NW * (uint32_t)row_bytes;
+      sc += 8 * NW * 4;
+      dst += 8 * NW * 128;
+    }
+    if (--steps > 0) fetch(h);
+    if constexpr (FMT == QUOKA_KV_MXFP8) {
+      *reinterpret_cast<uint4*>(to) = mx_to_bf16x8<FMT, PLAIN>(now.x, now.y, f);
+      *reinterpret_cast<uint4*>(to + (int)second) = mx_to_bf16x8<FMT, PLAIN>(now.z, now.w, f);
+    } else {
+      *reinterpret_cast<uint4*>(to) = mx_to_bf16x8<FMT, PLAIN>(now.x, 0u, f);
+      *reinterpret_cast<uint4*>(to + (int)second) = mx_to_bf16x8<FMT, PLAIN>(now.y, 0u, f);
+    }
+    if (steps <= 0) break;
+  }
+}
+
+// mbarrier: more bytes to come, without an arrival
+__device__ __forceinline__ void mbar_expect_tx(uint64_t* bar, uint32_t bytes) {
+  asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(smem_u32(bar)), "r"(bytes) : "memory");
+}
 
 // Where row t of a (sequence, KV head) is: its place in units of 16 elements from the cache's first, and its index among the rows of
 // scales.  (The host refuses caches of 2^32 - 1 units or rows and more.)

@@ -27,12 +27,10 @@ using namespace ptx;
 
 constexpr int kTileKeys = 128;
 constexpr int kScoreThreads = 320;          // 10 warps: TMA, MMA, two epilogue groups of four
-// Over a microscaled cache four loader warps more, which bring the key rows in and convert them (mx_rows.cuh); warp 0 has Q-bar only.
+// Over a microscaled cache warp 0 brings raw key rows in, and four warps more convert them (mx_rows.cuh).
 constexpr int kScoreLoaders = 4, kScoreMxThreads = kScoreThreads + 32 * kScoreLoaders;
 template <int FMT, int D>
-using ScoreRows = MxItem<FMT, D, 128, D, kScoreLoaders, /*PLAIN=*/true>;
-template <int FMT, int D>
-constexpr uint32_t kScoreWarpStage = ScoreRows<FMT, D>::kRaw + (D == 128 ? 128 : 256);
+using ScoreRows = MxItem<FMT, D, 128, D>;
 constexpr uint32_t kTmemCols = 512;
 constexpr int kMaxStages = 8;
 
@@ -100,11 +98,11 @@ __device__ __forceinline__ long long total_tiles(const DevParams& P) {
   return t;
 }
 
-// head_dim / 64; format of the cache (0: bf16, tm_k), of a microscaled one (k) the items of raw rows on their way
+// head_dim / 64; format of the cache (0: bf16), of a microscaled one the items of raw rows on their way
 template <int HALVES, int FMT = 0, int NST = 0>
 __global__ void __launch_bounds__(FMT != 0 ? kScoreMxThreads : kScoreThreads, 1)
 score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorMap tm_q,
-                     const __grid_constant__ CUtensorMap tm_k, const void* __restrict__ k, float* __restrict__ scores) {
+                     const __grid_constant__ CUtensorMap tm_k, float* __restrict__ scores) {
   constexpr bool MX = FMT != 0;
   constexpr uint32_t kHalfBytes = kTileKeys * 128;             // one 64-column half of a K tile
   constexpr uint32_t kStageBytes = HALVES * kHalfBytes;
@@ -120,7 +118,9 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
   uint64_t* acc_empty = acc_full + 2;          // [2]
   uint64_t* q_full = acc_empty + 2;
   uint64_t* q_empty = q_full + 1;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(q_empty + 1);
+  uint64_t* raw_full = q_empty + 1;            // MX: [NST] raw key rows are in
+  uint64_t* raw_empty = raw_full + NST;        // MX: [NST] and converted
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(raw_empty + NST);
   __shared__ int abort_flag;
 
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -132,9 +132,11 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
     for (int i = 0; i < 2; ++i) { mbar_init(&acc_full[i], 1); mbar_init(&acc_empty[i], 4); }
     mbar_init(q_full, 1);
     mbar_init(q_empty, 1);
+    if constexpr (MX)
+      for (int i = 0; i < NST; ++i) { mbar_init(&raw_full[i], 2); mbar_init(&raw_empty[i], kScoreLoaders); }
     fence_mbar_init();
     tma_prefetch_desc(&tm_q);
-    if (!MX) tma_prefetch_desc(&tm_k);
+    tma_prefetch_desc(&tm_k);
   }
   if (warp == 1) tmem_alloc(tmem_slot, kTmemCols);
   tc_fence_before();
@@ -150,7 +152,75 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
   const long long lo = total * blockIdx.x / gridDim.x, hi = total * (blockIdx.x + 1) / gridDim.x;
   const int slots = 2 / A.n_parts;
 
-  if (warp == 0) {
+  if (MX && warp == 0) {
+    // ------------------------------------------------------------------ microscaled cache: raw key rows, and Q-bar.  Rows past a sequence
+    // come in as they are, or as zeros past the cache: what becomes of them is not written.
+    if constexpr (MX) {
+      typedef ScoreRows<FMT, 64 * HALVES> Rows;
+      unsigned char* raw = reinterpret_cast<unsigned char*>(bars) + 1024;
+      MxPlaces places(P);
+      TileWalk w; w.seek(P, lo, hi);
+      int at = 0, head_cur = -1, q_deferred = -1, n_issued = 0; uint32_t phase = 0, qe_phase = 0;
+      bool waited = false;
+      const auto load_q = [&](int head) {
+        if (!waited) { grid_dependency_wait(); waited = true; }
+        if (lane == 0) {
+          mbar_arrive_expect_tx(q_full, (uint32_t)(HALVES * A.n_parts * A.box_rows * 128));
+          for (int h = 0; h < HALVES; ++h)
+            for (int p = 0; p < A.n_parts; ++p)
+              tma_load_3d(q_smem + (size_t)h * q_half_bytes + (size_t)p * A.box_rows * 128, &tm_q, q_full, h * 64, p * A.box_rows, head);
+        }
+      };
+      // the scale words of a tile, four rows a lane, a tile ahead
+      uint32_t word[4];
+      const auto ask = [&]() {
+        const int T_s = __ldg(P.ctx_len + w.s);
+        places.at_head(P, w.s, w.kv);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int t = w.tile * kTileKeys + 32 * i + lane;
+          uint32_t place, srow;
+          places.of(P, t < T_s ? t : -1, place, srow);
+          word[i] = t < T_s ? Rows::load_scales(P.k_scale, srow) : 0u;
+        }
+      };
+      if (w.valid()) ask();
+      while (w.valid()) {
+        const int head = w.s * P.n_kv + w.kv;
+        if (head != head_cur) {
+          if (q_deferred >= 0) { load_q(q_deferred); q_deferred = -1; }
+          if (head_cur >= 0) { if (!mbar_wait(q_empty, qe_phase, wc)) break; qe_phase ^= 1; }
+          if (n_issued == 0 && A.defer_q) q_deferred = head; else load_q(head);
+          head_cur = head;
+        }
+        if (!mbar_wait(&raw_empty[at], phase ^ 1, wc)) break;
+        unsigned char* stage = raw + (size_t)at * Rows::kStage;
+        if (lane == 0) {
+          fence_proxy_async_smem();                   // earlier contents of the stage were read through the generic proxy
+          mbar_arrive_expect_tx(&raw_full[at], Rows::kRaw);
+#pragma unroll
+          for (int sub = 0; sub < 2; ++sub) {
+            int c1 = w.tile * kTileKeys + sub * 64, c3 = w.s;
+            if (P.page_size != 0) {
+              const int pi = c1 >> 6, page = pi < P.max_pages ? __ldg(places.table + pi) : 0;
+              c1 = 0; c3 = page < 0 ? 0 : page;
+            }
+            tma_load_4d(stage + sub * 64 * Rows::kRowBytes, &tm_k, &raw_full[at], 0, c1, w.kv, c3);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) Rows::put_scales(smem_u32(stage), 32 * i + lane, word[i]);
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&raw_full[at]);
+        if (++at == NST) { at = 0; phase ^= 1; }
+        w.next(P);
+        if (w.valid()) ask();
+        if (++n_issued >= NST && q_deferred >= 0) { load_q(q_deferred); q_deferred = -1; }
+      }
+      if (q_deferred >= 0) load_q(q_deferred);
+      if (!waited) grid_dependency_wait();
+    }
+  } else if (warp == 0) {
     // ------------------------------------------------------------------ TMA producer
     if (lane == 0) {
       TileWalk w; w.seek(P, lo, hi);
@@ -168,16 +238,6 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
             tma_load_3d(q_smem + (size_t)h * q_half_bytes + (size_t)p * A.box_rows * 128, &tm_q, q_full, h * 64,
                         p * A.box_rows, head);
       };
-      if constexpr (MX) {                             // Q-bar alone
-        for (; w.valid(); w.next(P)) {
-          const int head = w.s * P.n_kv + w.kv;
-          if (head == head_cur) continue;
-          if (head_cur >= 0) { if (!mbar_wait(q_empty, qe_phase, wc)) break; qe_phase ^= 1; }
-          load_q(head);
-          head_cur = head;
-        }
-        if (!waited) grid_dependency_wait();
-      } else {
       for (; w.valid(); w.next(P)) {
         const int head = w.s * P.n_kv + w.kv;
         if (head != head_cur) {
@@ -209,47 +269,24 @@ score_keys_tc_kernel(DevParams P, ScoreArgs A, const __grid_constant__ CUtensorM
       if (q_deferred >= 0) load_q(q_deferred);
       // a CTA without tiles still waits: the chain of a fused call is only transitive if every link has waited
       if (!waited) grid_dependency_wait();
-      }
     }
   } else if (MX && warp >= kScoreThreads / 32) {
-    // ------------------------------------------------------------------ microscaled cache: key rows in, converted
+    // ------------------------------------------------------------------ microscaled cache: key rows converted
     if constexpr (MX) {
       typedef ScoreRows<FMT, 64 * HALVES> Rows;
-      constexpr uint32_t kWarpStage = kScoreWarpStage<FMT, 64 * HALVES>;
-      const int lw = warp - kScoreThreads / 32, my_row = Rows::row(lw, lane);
-      const uint32_t stage0 = smem_u32(reinterpret_cast<unsigned char*>(bars) + 1024) + (uint32_t)lw * (NST * kWarpStage);
-      MxPlaces places(P);
-      TileWalk in; in.seek(P, lo, hi);
-      TileWalk w = in;
-      const auto copy = [&](int at) {                 // the next tile's rows (keys past the sequence are zeros, their scores are not written)
-        if (in.valid()) {
-          const int t = in.tile * kTileKeys + my_row;
-          uint32_t place, srow;
-          places.at_head(P, in.s, in.kv);
-          places.of(P, t < __ldg(P.ctx_len + in.s) ? t : -1, place, srow);
-          const uint32_t raw = stage0 + (uint32_t)at * kWarpStage;
-          Rows::copy(static_cast<const typename Rows::W*>(k), place, P.k_scale, srow, raw, raw + Rows::kRaw, lane);
-          in.next(P);
-        }
-        cp_async_commit();
-      };
-#pragma unroll
-      for (int i = 0; i < NST; ++i) copy(i);
-      int stage = 0, at = 0; uint32_t phase = 0;
-      for (; w.valid(); w.next(P)) {
-        cp_async_wait<NST - 1>();
-        __syncwarp();
-        if (!mbar_wait(&empty[stage], phase ^ 1, wc)) break;
-        const uint32_t raw = stage0 + (uint32_t)at * kWarpStage;
-        Rows::convert(raw, Rows::scales(raw + Rows::kRaw, lane), 0, kBf16Nan2, k_smem + (size_t)stage * kStageBytes, lw, lane);
+      const uint32_t raw = smem_u32(reinterpret_cast<unsigned char*>(bars) + 1024);
+      int stage = 0, at = 0; uint32_t phase = 0, raw_phase = 0;
+      for (long long i = lo; i < hi; ++i) {
+        if (!mbar_wait(&raw_full[at], raw_phase, wc) || !mbar_wait_done(&empty[stage], phase ^ 1, wc)) break;
+        mx_convert<FMT, kScoreLoaders, /*PLAIN=*/true>(raw + (uint32_t)at * Rows::kStage, raw + (uint32_t)at * Rows::kStage + Rows::kRaw, kTileKeys, HALVES,
+                                                       Rows::kRowBytes, kBf16Nan2, k_smem + (size_t)stage * kStageBytes, kHalfBytes,
+                                                       warp - kScoreThreads / 32, lane);
         fence_proxy_async_smem();                     // these stores, before products read the stage
         __syncwarp();
-        if (lane == 0) mbar_arrive(&full[stage]);
-        copy(at);
-        if (++at == NST) at = 0;
+        if (lane == 0) { mbar_arrive(&full[stage]); mbar_arrive(&raw_empty[at]); }
+        if (++at == NST) { at = 0; raw_phase ^= 1; }
         if (++stage == A.stages) { stage = 0; phase ^= 1; }
       }
-      cp_async_wait_all();
     }
   } else if (warp == 1) {
     // ------------------------------------------------------------------ MMA issuer (the whole warp, one lane issues)
@@ -455,6 +492,18 @@ bool encode_kv_tensor_map(CUtensorMap* out, const quoka_params* p, const void* c
   return encode_tensor_map_bf16(out, cache, 4, dims, strides, box);
 }
 
+bool encode_mx_tensor_map(CUtensorMap* out, const quoka_params* p, int fmt, const void* cache, int cols) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  const int bits = fmt == QUOKA_KV_MXFP8 ? 8 : 4;
+  const cuuint64_t dims[4] = {(cuuint64_t)p->head_dim * bits / 8, (cuuint64_t)(p->page_size ? kPage : p->kv_rows), (cuuint64_t)p->n_kv_heads,
+                              (cuuint64_t)(p->page_size ? p->kv_rows : p->batch)};
+  const cuuint64_t strides[3] = {(cuuint64_t)p->kv_stride_t * bits / 8, (cuuint64_t)p->kv_stride_h * bits / 8, (cuuint64_t)p->kv_stride_b * bits / 8};
+  const cuuint32_t box[4] = {(cuuint32_t)(cols * bits / 8), 64, 1, 1}, one[4] = {1, 1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(cache), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE,
+            CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool score_keys_tc_supported(const quoka_params* p) {
   if (p->dtype != QUOKA_BF16) return false;
   const int N = p->n_retain < p->chunk_len ? p->n_retain : p->chunk_len;
@@ -465,10 +514,10 @@ bool score_keys_tc_supported(const quoka_params* p) {
 
 template <typename Kernel>
 static cudaError_t launch_score(Kernel kernel, const char* name, int grid, int threads, size_t smem, cudaStream_t st, bool chained, const DevParams& P,
-                                const ScoreArgs& A, const CUtensorMap& tm_q, const CUtensorMap& tm_k, const void* k, float* scores) {
+                                const ScoreArgs& A, const CUtensorMap& tm_q, const CUtensorMap& tm_k, float* scores) {
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_kernel(name, kernel, dim3(grid), dim3(threads), smem, st, 1, chained, P, A, tm_q, tm_k, k, scores);
+  e = launch_kernel(name, kernel, dim3(grid), dim3(threads), smem, st, 1, chained, P, A, tm_q, tm_k, scores);
   if (e == cudaSuccess) count_launch();
   return e;
 }
@@ -493,7 +542,7 @@ quoka_status launch_score_keys_tc(const quoka_params* p, const DevParams& P, con
   if (max_tiles < grid) grid = (int)max_tiles;
   if (grid <= 0) return QUOKA_OK;
   const cudaError_t e = launch_score(P.d == 128 ? score_keys_tc_kernel<2> : score_keys_tc_kernel<1>, "score_keys_tc", grid, kScoreThreads, pl.total, st, chained, P,
-                                     A, tm_q, tm_k, nullptr, scores);
+                                     A, tm_q, tm_k, scores);
   return (e == cudaSuccess && cudaGetLastError() == cudaSuccess) ? QUOKA_OK : QUOKA_ERR_CUDA;
 }
 
@@ -503,17 +552,18 @@ quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, 
                                      bool chained) {
   const int N = P.n_sel;
   // Three items of raw rows on their way, one where the retained queries (more than 256 at head_dim 128) leave no room for them.
-  const size_t item = kScoreLoaders * (P.d == 128 ? (fmt == QUOKA_KV_MXFP8 ? kScoreWarpStage<QUOKA_KV_MXFP8, 128> : kScoreWarpStage<QUOKA_KV_MXFP4, 128>)
-                                                  : (fmt == QUOKA_KV_MXFP8 ? kScoreWarpStage<QUOKA_KV_MXFP8, 64> : kScoreWarpStage<QUOKA_KV_MXFP4, 64>));
+  const size_t item = P.d == 128 ? (fmt == QUOKA_KV_MXFP8 ? ScoreRows<QUOKA_KV_MXFP8, 128>::kStage : ScoreRows<QUOKA_KV_MXFP4, 128>::kStage)
+                                 : (fmt == QUOKA_KV_MXFP8 ? ScoreRows<QUOKA_KV_MXFP8, 64>::kStage : ScoreRows<QUOKA_KV_MXFP4, 64>::kStage);
   const bool three = plan_score_smem(N, P.d, 3 * item).stages >= 3;
   const ScoreSmemPlan pl = plan_score_smem(N, P.d, (three ? 3 : 1) * item);
   if (pl.stages < 2) return QUOKA_ERR_UNSUPPORTED;
-  CUtensorMap tm_q, none = {};
+  CUtensorMap tm_q, tm_k;
+  if (!encode_mx_tensor_map(&tm_k, p, fmt, k, P.d)) return QUOKA_ERR_CUDA;
   const uint64_t dims[3] = {(uint64_t)P.d, (uint64_t)N, (uint64_t)P.batch * P.n_kv};
   const uint64_t strides[2] = {(uint64_t)P.d * 2, (uint64_t)N * P.d * 2};
   const uint32_t box[3] = {64, (uint32_t)pl.box_rows, 1};
   if (!encode_tensor_map_bf16(&tm_q, qbar, 3, dims, strides, box)) return QUOKA_ERR_CUDA;
-  ScoreArgs A{N, pl.n_pad, pl.n_parts, pl.box_rows, pl.q_rows, pl.stages, 0};
+  ScoreArgs A{N, pl.n_pad, pl.n_parts, pl.box_rows, pl.q_rows, pl.stages, chained ? 1 : 0};
   const long long max_tiles = (long long)P.batch * P.n_kv * ((P.max_ctx + kTileKeys - 1) / kTileKeys);
   int grid = device_sm_count();
   if (grid <= 0) return QUOKA_ERR_CUDA;
@@ -522,7 +572,7 @@ quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, 
   const cudaError_t e = mx_dispatch(QUOKA_BF16, fmt, P.d, [&](auto, auto f, auto d) {
     constexpr int FMT = decltype(f)::value, H = decltype(d)::value / 64;
     return launch_score(three ? score_keys_tc_kernel<H, FMT, 3> : score_keys_tc_kernel<H, FMT, 1>, "score_keys_mx_tc", grid, kScoreMxThreads, pl.total, st, chained,
-                        P, A, tm_q, none, k, scores);
+                        P, A, tm_q, tm_k, scores);
   });
   return (e == cudaSuccess && cudaGetLastError() == cudaSuccess) ? QUOKA_OK : QUOKA_ERR_CUDA;
 }

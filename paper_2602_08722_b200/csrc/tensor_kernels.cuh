@@ -1,6 +1,8 @@
 // Host-side entry points of the tcgen05 (5th-generation tensor core) kernels.
 #pragma once
 
+#include <cuda.h>
+
 #include "common.cuh"
 
 namespace quoka {
@@ -40,6 +42,8 @@ quoka_status launch_attn_tc_pair(const quoka_params* p, const DevParams& P, cons
                                  bool after_selection, const AttnPlan& plan);
 
 // The same over a microscaled cache (the scale arrays in P).
+// raw rows of the cache, `cols` columns, in boxes of 64 rows
+bool encode_mx_tensor_map(CUtensorMap* out, const quoka_params* p, int fmt, const void* cache, int cols);
 bool score_keys_mx_tc_supported(const quoka_params* p);
 quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st,
                                      bool chained);
