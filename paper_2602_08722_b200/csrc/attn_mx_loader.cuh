@@ -24,15 +24,8 @@ constexpr int kMxAttnThreads = 512, kMxLoaderWarps = 4, kMxFirstLoader = 12;
 constexpr int kMxSoftmaxRegs = 168, kMxOtherRegs = 88;
 static_assert(256 * kMxSoftmaxRegs + 256 * kMxOtherRegs == kMxAttnThreads * 128, "what the block is launched with");
 
-constexpr int kNoNan = 0x7FFFFFFF;
 
-// 8 bf16 numbers in plain order, put in that order.
-template <int FMT>
-__device__ __forceinline__ uint4 mx_order(uint4 w) {
-  const uint32_t a = FMT == QUOKA_KV_MXFP8 ? w.y : w.z, b = FMT == QUOKA_KV_MXFP8 ? w.z : w.y;     // what goes with x, and with w
-  return make_uint4(__byte_perm(w.x, a, 0x5410), __byte_perm(w.x, a, 0x7632), __byte_perm(b, w.w, 0x5410), __byte_perm(b, w.w, 0x7632));
-}
-// The CTA's Q tiles in that order, in place, by the converting warps before their first item; `ready` gets an arrival of each warp.
+// The CTA's Q tiles in the order of converted rows, in place, by the converting warps before their first item; `ready` gets an arrival of each warp.
 template <int FMT>
 __device__ __forceinline__ bool mx_order_q(unsigned char* q_smem, int bytes, int thread, int threads, uint64_t* q_full, uint64_t* ready, const WaitCtx& wc) {
   if (!mbar_wait(q_full, 0, wc)) return false;

@@ -1,0 +1,572 @@
+// Attention of a few query rows per KV head over a microscaled cache: generation steps, and the few positions of a speculated
+// continuation.  The C chunk positions of the G heads of a KV group are R = C G query rows, taken 8 or 16 at a time.
+//
+// What bounds it: HBM (every row of the cache is read once and used for a dozen multiplications), and next to it the instructions
+// that turn 8 or 4 bits into operands.  So the products are matrix instructions with the keys on the M side (m16n8k16: the query
+// rows fill the 8 columns, a 128-row tcgen05 tile would have 4 or 8 rows of use in 128), whose operands a lane builds in registers from the
+// bytes it copied itself:
+//   S^T = K Q^T   a lane brings 16-byte pieces of two key rows; which columns they are does not matter to the sum, Q's fragment has the same
+//   O^T = V^T P^T a lane brings the same 8 or 16 columns of four value rows and interleaves the rows of a pair
+// P^T comes out of S^T by an 8 x 8 transposition (movmatrix).  Nothing but the scale words crosses lanes on the way in.
+//
+// Split: the 16-key granules of all (sequence, KV head, row group) in one list, cut into equal contiguous shares, one per CTA; inside a
+// CTA the warps take granules in turn, each with a running maximum, sum and output of its own, added up at the end of a unit's part.
+// A unit that several CTAs share is added up by a second kernel, part by part in order.  Long lists are balanced whatever the
+// sequences' lengths are.  Weights are rounded to bf16 for the product and divided by their sum as rounded, so that they add up to
+// one; the log-sum-exp is that of the weights before.
+#include <algorithm>
+
+#include "mx_host.cuh"
+#include "mx_rows.cuh"
+#include "tensor_kernels.cuh"
+
+namespace quoka {
+
+using namespace ptx;
+
+constexpr int kDecGranule = 16;
+
+template <int NT> constexpr int kDecWarps = NT == 1 ? 12 : 8;
+constexpr int kDecStages = 3;
+
+// What a lane copies of a granule: K_PIECES pieces of K_BYTES of each of two rows, V_BYTES of each of four.
+template <int FMT, int D>
+struct DecBytes {
+  static constexpr int kRow = D * kMxBits<FMT> / 8;
+  static constexpr int kKPieces = kRow == 128 ? 2 : 1, kKBytes = kRow / 4 / kKPieces, kVBytes = kRow / 8;
+  static constexpr uint32_t kK = 2 * kKPieces * 32 * kKBytes, kV = 4 * 32 * kVBytes;
+  static constexpr uint32_t kStage = kK + kV + (D == 128 ? 128 : 256);       // scale words of 16 rows of K and of V, head_dim 64 also their shifts
+  static_assert(kK == kDecGranule * kRow && kV == kDecGranule * kRow, "a granule");
+};
+
+template <int BYTES>
+__device__ __forceinline__ void cp_async_n(uint32_t dst, const void* src, bool valid) {
+  if constexpr (BYTES == 16) {
+    cp_async_16(dst, src, valid);
+  } else {
+    const uint32_t n = valid ? (uint32_t)BYTES : 0u;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %3, %2;" ::"r"(dst), "l"(src), "r"(n), "n"(BYTES) : "memory");
+  }
+}
+template <int WORDS>
+__device__ __forceinline__ void lds_words(uint32_t at, uint32_t* w) {
+  if constexpr (WORDS == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at) : "memory");
+  else if constexpr (WORDS == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+
+// The list of granules: unit = (sequence, KV head, row group), in this order.
+struct DecWork {
+  int groups;              // row groups of a KV head
+  const int32_t* k_cnt;    // listed: rows in the list (device), or null
+  // keys of a sequence: cached (listed or all), then the chunk's own
+  __device__ __forceinline__ int cached(const DevParams& P, int s) const { return k_cnt ? __ldcg(k_cnt + s) : load_input<true>(P.ctx_len + s); }
+  __device__ __forceinline__ int granules(const DevParams& P, int s) const { return (cached(P, s) + P.chunk + kDecGranule - 1) / kDecGranule; }
+  // granules of sequences [0, s), s <= batch (whole warp)
+  __device__ __forceinline__ long long before(const DevParams& P, int s, int lane) const {
+    long long sum = 0;
+    for (int s0 = 0; s0 < s; s0 += 32) sum += __reduce_add_sync(0xFFFFFFFFu, s0 + lane < s ? granules(P, s0 + lane) : 0);
+    return sum * (P.n_kv * groups);
+  }
+};
+// A CTA's share of the list, part of a unit after part of a unit; identical in every warp.
+struct DecPart {
+  int s, kv, grp;          // unit
+  int cnt, n;              // its cached keys and its granules
+  int begin, end;          // granules of this part
+  long long left;          // granules of the share behind this part
+  __device__ __forceinline__ void seek(const DevParams& P, const DecWork& w, long long lo, long long hi, int lane) {
+    left = hi - lo;
+    s = 0;
+    const int heads = P.n_kv * w.groups;
+    for (;; s += 32) {                                // the sequence that lo is in
+      const long long mine = s + lane < P.batch ? (long long)w.granules(P, s + lane) * heads : 0;
+      long long incl = mine;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += v;
+      }
+      const uint32_t hit = __ballot_sync(0xFFFFFFFFu, incl > lo);
+      if (hit != 0) {
+        const int src = __ffs(hit) - 1;
+        lo -= __shfl_sync(0xFFFFFFFFu, incl - mine, src);
+        s += src;
+        break;
+      }
+      lo -= __shfl_sync(0xFFFFFFFFu, incl, 31);
+    }
+    set(P, w);
+    const int unit = (int)(lo / n);
+    kv = unit / w.groups;
+    grp = unit % w.groups;
+    begin = (int)(lo % n);
+    cut();
+  }
+  __device__ __forceinline__ void set(const DevParams& P, const DecWork& w) {
+    cnt = w.cached(P, s);
+    n = (cnt + P.chunk + kDecGranule - 1) / kDecGranule;
+  }
+  __device__ __forceinline__ void cut() {
+    end = (int)min((long long)n, begin + left);
+    left -= end - begin;
+  }
+  // false: that was the last
+  __device__ __forceinline__ bool next(const DevParams& P, const DecWork& w) {
+    if (left <= 0) { begin = end; return false; }
+    if (++grp == w.groups) {
+      grp = 0;
+      if (++kv == P.n_kv) { kv = 0; ++s; set(P, w); }
+    }
+    begin = 0;
+    cut();
+    return true;
+  }
+};
+
+template <int FMT, int D, int NT>
+__global__ void __launch_bounds__(32 * kDecWarps<NT>, 1)
+decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
+                 const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units) {
+  typedef DecBytes<FMT, D> B;
+  constexpr int WARPS = kDecWarps<NT>, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
+  constexpr int KW = B::kKBytes * B::kKPieces / 4, VW = B::kVBytes / 4;      // words of a lane per row
+  constexpr int LD = D + 4;                                                  // floats of a row of the merge buffer
+  extern __shared__ __align__(16) unsigned char dec_smem[];
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
+  const uint32_t ring = smem_u32(dec_smem) + (uint32_t)warp * (ST * B::kStage);
+  float* merge = reinterpret_cast<float*>(dec_smem + (size_t)WARPS * ST * B::kStage);        // [WARPS][ROWS][LD], then m, l, lx [WARPS][ROWS]
+  float* merge_ml = merge + WARPS * ROWS * LD;
+  // ---- this CTA's share
+  long long lo, hi;
+  if (whole_units) {                                  // one unit per CTA
+    const int unit = blockIdx.x, per_s = P.n_kv * work.groups, s = unit / per_s;
+    const int n = work.granules(P, s);
+    lo = work.before(P, s, lane) + (long long)(unit % per_s) * n;
+    hi = lo + n;
+  } else {
+    const long long total = work.before(P, P.batch, lane);
+    lo = total * blockIdx.x / gridDim.x;
+    hi = total * (blockIdx.x + 1) / gridDim.x;
+  }
+  if (lo >= hi) return;
+  DecPart in;
+  in.seek(P, work, lo, hi, lane);
+  DecPart part = in;
+  // ---- copies: granules begin + warp, + WARPS .. of every part.  Lanes 0-15 look after a row's keys, 16-31 after its values: row numbers
+  // two granules ahead, places one ahead.
+  MxPlaces places(P);
+  int pos = in.begin + warp;
+  bool more = true;
+  const auto settle = [&]() { while (more && pos >= in.end) { more = in.next(P, work); pos = in.begin + warp; } };
+  const auto row_number = [&]() -> int {              // of this lane's row in granule pos, -1: none
+    if (!more) return -1;
+    const int u = pos * kDecGranule + (lane & 15);
+    if (u >= in.cnt + P.chunk) return -1;
+    if (u >= in.cnt) return load_input<true>(P.ctx_len + in.s) + (u - in.cnt);
+    return k_idx ? __ldcg(k_idx + ((long long)in.s * P.n_kv + in.kv) * P.budget_cap + u) : u;
+  };
+  int t_next, s_next = 0, kv_next = 0;                // of the granule whose places are worked out next
+  bool live_next = false;
+  uint32_t place = kNoRow, srow = 0;                  // of the granule that is copied next
+  bool live = false;
+  const auto ask = [&]() {
+    settle();
+    live_next = more;
+    s_next = in.s; kv_next = in.kv;
+    t_next = row_number();
+    pos += WARPS;
+  };
+  const auto locate = [&]() {
+    live = live_next;
+    int t = t_next;
+#ifdef QUOKA_DEBUG
+    if (live && (t < -1 || t >= __ldg(P.ctx_len + s_next) + P.chunk)) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
+#endif
+    places.at_head(P, s_next, kv_next);
+    places.of(P, live ? t : -1, place, srow);
+  };
+  const auto fill = [&](int stage) {
+    if (live) {
+      const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV + 4 * lane;
+      const uint8_t* sc = lane < 16 ? P.k_scale : P.v_scale;
+      if (place != kNoRow) cp_async_4(meta, sc + (D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4));
+      else asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta), "r"(0u) : "memory");
+      if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 128), "r"((srow & 1u) * 16) : "memory");
+      constexpr int kUnit = 2 * kMxBits<FMT>;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, g + 8 * i);
+        const uint8_t* src = kc + (size_t)(row == kNoRow ? 0u : row) * kUnit + c * B::kKBytes;
+#pragma unroll
+        for (int p = 0; p < B::kKPieces; ++p)          // (pieces 64 bytes apart: a warp asks for every sector once)
+          cp_async_n<B::kKBytes>(at + (uint32_t)((i * B::kKPieces + p) * 32 + lane) * B::kKBytes, src + 64 * p, row != kNoRow);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, 2 * c + (i & 1) + 8 * (i >> 1));
+        cp_async_n<B::kVBytes>(at + B::kK + (uint32_t)(i * 32 + lane) * B::kVBytes, vc + (size_t)(row == kNoRow ? 0u : row) * kUnit + g * B::kVBytes, row != kNoRow);
+      }
+    }
+    cp_async_commit();
+    locate();
+    ask();
+  };
+  ask();
+  locate();
+  ask();
+#pragma unroll
+  for (int i = 0; i < ST; ++i) fill(i);
+
+  const float scale_log2 = P.scale * 1.4426950408889634f * kMxUnshift;
+  uint32_t qf[NT][2 * KSTEPS];
+  float o[NT][TILES][4], m[NT][2], l[NT][2], lx[NT][2];    // lx: the sum of the weights before they are rounded
+  int stage = 0, s_cur = -1, kv_cur = -1, grp_cur = -1;
+  for (bool again = true; again;) {
+    const int first_row = part.grp * ROWS, n_rows = min(ROWS, P.chunk * P.group - first_row);
+    // ---- the part's query rows, in the order of the converted keys
+    if (part.s != s_cur || part.kv != kv_cur || part.grp != grp_cur) {
+      s_cur = part.s; kv_cur = part.kv; grp_cur = part.grp;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const int row = 8 * nt + g, r = first_row + row;
+        const __nv_bfloat16* qr = q + (long long)part.s * P.q_sb + (long long)(part.kv * P.group + r % P.group) * P.q_sh + (long long)(r / P.group) * P.q_st;
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {             // 8 columns of the lane's D / 4
+          const int col = FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j;
+          uint4 w = make_uint4(0, 0, 0, 0);
+          if (row < n_rows) w = load_input<true>(reinterpret_cast<const uint4*>(qr + col));
+          w = mx_order<FMT>(w);
+          qf[nt][4 * j] = w.x; qf[nt][4 * j + 1] = w.y; qf[nt][4 * j + 2] = w.z; qf[nt][4 * j + 3] = w.w;
+        }
+      }
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+      for (int e = 0; e < 2; ++e) { m[nt][e] = -INFINITY; l[nt][e] = lx[nt][e] = 0.f; }
+#pragma unroll
+      for (int t = 0; t < TILES; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[nt][t][e] = 0.f;
+    }
+    int nan_u = kNoNan;                                // first key, in the order of visibility, with a value that is not finite in this lane's columns
+    // keys that the rows of this lane's columns see: 2 c and 2 c + 1 of each tile
+    int sees[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) sees[nt][e] = part.cnt + min(first_row + 8 * nt + 2 * c + e, P.chunk * P.group - 1) / P.group + 1;
+    const int all_see = part.cnt + first_row / P.group + 1;         // keys that every row sees
+#pragma unroll 1
+    for (int gr = part.begin + warp; gr < part.end; gr += WARPS) {
+      cp_async_wait<ST - 1>();
+      __syncwarp();
+      const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV;
+      const auto scale_word = [&](int i) {
+        uint32_t w;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(meta + 4 * i) : "memory");
+        if (D == 64) {
+          uint32_t shift;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 128 + 4 * i) : "memory");
+          w = w >> shift & 0xFFFFu;
+        }
+        return w;
+      };
+      // ---- S^T = K Q^T
+      float sc[NT][4];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
+      {
+        uint32_t w0[KW], w1[KW];
+#pragma unroll
+        for (int p = 0; p < B::kKPieces; ++p) {
+          lds_words<B::kKBytes / 4>(at + (uint32_t)(p * 32 + lane) * B::kKBytes, w0 + p * (B::kKBytes / 4));
+          lds_words<B::kKBytes / 4>(at + (uint32_t)((B::kKPieces + p) * 32 + lane) * B::kKBytes, w1 + p * (B::kKBytes / 4));
+        }
+        const uint32_t sw0 = scale_word(g), sw1 = scale_word(g + 8);
+        // the lane's block(s): 32 columns from c * D / 4 on, two of 16 columns at 8 bits and head_dim 128
+        const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
+        const auto factor = [&](uint32_t word, int b) {
+          const uint32_t e = word >> (8 * b) & 0xFFu;
+          return e == kMxNanScale ? kBf16Nan2 : mx_factor2<FMT>(e);
+        };
+        uint32_t f0 = factor(sw0, blk), f1 = factor(sw1, blk);
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          if (B::kKPieces == 2 && j == KW / 2) { f0 = factor(sw0, blk + 2); f1 = factor(sw1, blk + 2); }
+          if constexpr (FMT == QUOKA_KV_MXFP8) {
+            uint32_t a[2], b[2];
+            mx_to_pairs<FMT>(w0[j], f0, a);
+            mx_to_pairs<FMT>(w1[j], f1, b);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) mma_bf16(sc[nt], a[0], b[0], a[1], b[1], qf[nt][2 * j], qf[nt][2 * j + 1]);
+          } else {
+            uint32_t a[4], b[4];
+            mx_to_pairs<FMT>(w0[j], f0, a);
+            mx_to_pairs<FMT>(w1[j], f1, b);
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+              mma_bf16(sc[nt], a[0], b[0], a[1], b[1], qf[nt][4 * j], qf[nt][4 * j + 1]);
+              mma_bf16(sc[nt], a[2], b[2], a[3], b[3], qf[nt][4 * j + 2], qf[nt][4 * j + 3]);
+            }
+          }
+        }
+      }
+      // ---- softmax: a lane has keys g and g + 8 of rows 2 c and 2 c + 1
+      const int u0 = gr * kDecGranule;
+      if (u0 + kDecGranule > all_see) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (u0 + g + 8 * (e >> 1) >= sees[nt][e & 1]) sc[nt][e] = -INFINITY;
+      }
+      bool grow = false;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) grow |= fmaxf(sc[nt][e], sc[nt][e + 2]) * scale_log2 > m[nt][e] + kRescaleThreshold;
+      if (__any_sync(0xFFFFFFFFu, grow)) {              // (the reference point of the exponentials moves by more than 2^32, or is set)
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            float mx = fmaxf(m[nt][e], fmaxf(sc[nt][e], sc[nt][e + 2]) * scale_log2);
+#pragma unroll
+            for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, sh));
+            const float alpha = m[nt][e] == mx ? 1.f : ex2(m[nt][e] - mx);
+            m[nt][e] = mx;
+            l[nt][e] *= alpha;
+            lx[nt][e] *= alpha;
+#pragma unroll
+            for (int t = 0; t < TILES; ++t) { o[nt][t][e] *= alpha; o[nt][t][e + 2] *= alpha; }
+          }
+      }
+      uint32_t pf[NT][2];
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const float p0 = ex2(fmaf(sc[nt][2 * h], scale_log2, -m0)), p1 = ex2(fmaf(sc[nt][2 * h + 1], scale_log2, -m1));
+          const __nv_bfloat162 p2 = __floats2bfloat162_rn(p0, p1);
+          lx[nt][0] += p0;
+          lx[nt][1] += p1;
+          const uint32_t w = *reinterpret_cast<const uint32_t*>(&p2);
+          l[nt][0] += __uint_as_float(w << 16);
+          l[nt][1] += __uint_as_float(w & 0xFFFF0000u);
+          pf[nt][h] = transpose8x8(w);
+        }
+      }
+      // ---- O^T += V^T P^T
+      {
+        uint32_t f[2];
+        const int blk = D == 128 ? g >> 1 : g >> 2;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t e0 = scale_word(16 + 2 * c + 8 * h) >> (8 * blk) & 0xFFu, e1 = scale_word(17 + 2 * c + 8 * h) >> (8 * blk) & 0xFFu;
+          if (e0 == kMxNanScale) nan_u = min(nan_u, u0 + 2 * c + 8 * h);
+          if (e1 == kMxNanScale) nan_u = min(nan_u, u0 + 2 * c + 8 * h + 1);
+          f[h] = (e0 == kMxNanScale ? 0u : mx_factor2<FMT>(e0) & 0xFFFFu) | (e1 == kMxNanScale ? 0u : mx_factor2<FMT>(e1) & 0xFFFF0000u);
+        }
+        uint32_t v[4][VW];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kK + (uint32_t)(i * 32 + lane) * B::kVBytes, v[i]);
+#pragma unroll
+        for (int w = 0; w < VW; ++w) {
+          // columns of the word, the two rows of a pair side by side: 2 (4 bits: 4) and as many
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            constexpr int N = FMT == QUOKA_KV_MXFP8 ? 2 : 4;
+            uint32_t x[N], y[N];
+            mx_to_pairs<FMT>(__byte_perm(v[0][w], v[1][w], h ? 0x7632 : 0x5410), f[0], x);
+            mx_to_pairs<FMT>(__byte_perm(v[2][w], v[3][w], h ? 0x7632 : 0x5410), f[1], y);
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+                mma_bf16(o[nt][(w * 2 + h) * (N / 2) + i], x[2 * i], x[2 * i + 1], y[2 * i], y[2 * i + 1], pf[nt][0], pf[nt][1]);
+          }
+        }
+      }
+      __syncwarp();                                    // the scale words of this stage have been read
+      fill(stage);
+      if (++stage == ST) stage = 0;
+    }
+    // ---- the warps' results of this part
+    nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 1));
+    nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 2));
+    __syncthreads();                                   // (the buffer's last part has been read)
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float sum = l[nt][e], sumx = lx[nt][e];
+#pragma unroll
+        for (int sh = 4; sh < 32; sh <<= 1) {
+          sum += __shfl_xor_sync(0xFFFFFFFFu, sum, sh);
+          sumx += __shfl_xor_sync(0xFFFFFFFFu, sumx, sh);
+        }
+        const int row = 8 * nt + 2 * c + e;
+        if (g == 0) { merge_ml[warp * ROWS + row] = m[nt][e]; merge_ml[(WARPS + warp) * ROWS + row] = sum; merge_ml[(2 * WARPS + warp) * ROWS + row] = sumx; }
+        const bool bad = nan_u < sees[nt][e];
+        float2* to = reinterpret_cast<float2*>(merge + (warp * ROWS + row) * LD + g * (D / 8));
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+          const float bad_value = __uint_as_float(0x7FC00000u);
+          to[t] = bad ? make_float2(bad_value, bad_value) : make_float2(o[nt][t][e], o[nt][t][e + 2]);
+        }
+      }
+    __syncthreads();
+    const bool is_whole = part.begin == 0 && part.end == part.n;
+    const int slot = blockIdx.x * 2 + (part.begin == 0 ? 1 : 0);
+    for (int i = threadIdx.x; i < n_rows * (D / 4); i += 32 * WARPS) {
+      const int row = i / (D / 4), col = i % (D / 4) * 4;
+      float mx = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, merge_ml[w * ROWS + row]);
+      float sum = 0.f, sumx = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int w = 0; w < WARPS; ++w) {
+        const float mw = merge_ml[w * ROWS + row], wt = mw == -INFINITY && mx != -INFINITY ? 0.f : mw == mx ? 1.f : ex2(mw - mx);
+        const float4 v = *reinterpret_cast<const float4*>(merge + (w * ROWS + row) * LD + col);
+        sum = fmaf(wt, merge_ml[(WARPS + w) * ROWS + row], sum);
+        sumx = fmaf(wt, merge_ml[(2 * WARPS + w) * ROWS + row], sumx);
+        acc.x = fmaf(wt, v.x, acc.x); acc.y = fmaf(wt, v.y, acc.y); acc.z = fmaf(wt, v.z, acc.z); acc.w = fmaf(wt, v.w, acc.w);
+      }
+      if (is_whole) {
+        const int r = first_row + row, h = part.kv * P.group + r % P.group, pos_r = r / P.group;
+        const float inv = kMxUnshift / sum;
+        const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), b = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+        *reinterpret_cast<uint2*>(out + (long long)part.s * P.o_sb + (long long)h * P.o_sh + (long long)pos_r * P.o_st + col) =
+            make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+        if (lse && col == 0) lse[((long long)part.s * P.n_q + h) * P.chunk + pos_r] = (mx + log2f(sumx)) * 0.6931471805599453f;
+      } else {
+        float* to = parts + (size_t)slot * ROWS * (D + 3);
+        *reinterpret_cast<float4*>(to + row * D + col) = acc;
+        if (col == 0) { to[ROWS * D + row] = mx; to[ROWS * (D + 1) + row] = sum; to[ROWS * (D + 2) + row] = sumx; }
+      }
+    }
+    again = part.next(P, work);
+  }
+  cp_async_wait_all();                                 // nothing of this thread is in flight at exit
+}
+
+// Units that several CTAs of the list share, a warp per query row: the parts added up in their order.
+template <int D, int NT>
+__global__ void __launch_bounds__(128) decode_mx_join_kernel(DevParams P, DecWork work, const float* __restrict__ parts, int ctas, __nv_bfloat16* __restrict__ out,
+                                                             float* __restrict__ lse) {
+  constexpr int ROWS = 8 * NT, PER = D / 32;
+  grid_dependency_wait();
+  grid_launch_dependents();
+  const int lane = threadIdx.x & 31, unit = blockIdx.x, per_s = P.n_kv * work.groups, s = unit / per_s;
+  const int row = blockIdx.y * 4 + (threadIdx.x >> 5), grp = unit % work.groups, r = grp * ROWS + row;
+  const int n = work.granules(P, s);
+  const long long total = work.before(P, P.batch, lane), a = work.before(P, s, lane) + (long long)(unit % per_s) * n, b = a + n;
+  if (row >= ROWS || r >= P.chunk * P.group) return;
+  // CTA i has [total i / ctas, total (i + 1) / ctas)
+  const auto cta_of = [&](long long at) {
+    long long i = at * ctas / total;
+    while (total * (i + 1) / ctas <= at) ++i;
+    while (total * i / ctas > at) --i;
+    return (int)i;
+  };
+  const int first = cta_of(a), last = cta_of(b - 1);
+  if (first == last) return;                           // (written by that CTA)
+  const auto slot = [&](int i) { return parts + (size_t)(2 * i + (i == first ? 1 : 0)) * ROWS * (D + 3); };
+  float mx = -INFINITY;
+  for (int i = first + lane; i <= last; i += 32) mx = fmaxf(mx, __ldcg(slot(i) + ROWS * D + row));
+#pragma unroll
+  for (int sh = 16; sh > 0; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, sh));
+  float sum = 0.f, sumx = 0.f, acc[PER];
+#pragma unroll
+  for (int e = 0; e < PER; ++e) acc[e] = 0.f;
+#pragma unroll 4
+  for (int i = first; i <= last; ++i) {
+    const float* p = slot(i);
+    const float mi = __ldcg(p + ROWS * D + row), wt = mi == -INFINITY && mx != -INFINITY ? 0.f : mi == mx ? 1.f : ex2(mi - mx);
+    sum = fmaf(wt, __ldcg(p + ROWS * (D + 1) + row), sum);
+    sumx = fmaf(wt, __ldcg(p + ROWS * (D + 2) + row), sumx);
+    float v[PER];
+    load_vec<float, PER, true>(p + row * D + lane * PER, v);
+#pragma unroll
+    for (int e = 0; e < PER; ++e) acc[e] = fmaf(wt, v[e], acc[e]);
+  }
+  const int h = unit % per_s / work.groups * P.group + r % P.group, pos = r / P.group;
+  const float inv = kMxUnshift / sum;
+#pragma unroll
+  for (int e = 0; e < PER; ++e) acc[e] *= inv;
+  store_vec<__nv_bfloat16, PER>(out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)pos * P.o_st + lane * PER, acc);
+  if (lse && lane == 0) lse[((long long)s * P.n_q + h) * P.chunk + pos] = (mx + log2f(sumx)) * 0.6931471805599453f;
+}
+
+// ---------------------------------------------------------------------------------------------- host
+static int dec_tiles(const DevParams& P) { return P.chunk * P.group <= 8 ? 1 : 2; }
+
+// Query rows that these kernels take.
+bool decode_mx_applies(const quoka_params* p) { return (long long)p->chunk_len * (p->n_q_heads / p->n_kv_heads) <= 16 || p->chunk_len == 1; }
+
+// Parts of the shared units: two slots a CTA, one CTA per SM.
+size_t decode_mx_scratch_bytes(const quoka_params* p) {
+  const int sms = device_sm_count() > 0 ? device_sm_count() : 148;
+  return (size_t)sms * 2 * 16 * (p->head_dim + 3) * sizeof(float);
+}
+
+template <int FMT, int D, int NT>
+static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt, void* out,
+                                      float* lse, float* parts, cudaStream_t st, bool chained) {
+  constexpr int WARPS = kDecWarps<NT>, ROWS = 8 * NT;
+  DecWork work;
+  work.groups = (P.chunk * P.group + ROWS - 1) / ROWS;
+  work.k_cnt = k_idx ? k_cnt : nullptr;
+  const int sms = device_sm_count();
+  if (sms <= 0) return cudaErrorInvalidDevice;
+  const long long units = (long long)P.batch * P.n_kv * work.groups;
+  const long long most = ((k_idx ? (long long)P.budget_cap : (long long)P.max_ctx) + P.chunk + kDecGranule - 1) / kDecGranule;      // granules of a unit
+  // A CTA per unit where that is three rounds of its warps or fewer, or where units are many: what joining parts costs (a launch, a
+  // round trip through L2) is more than what the shorter rounds gain.
+  const bool whole = most <= 3 * WARPS || units >= 64ll * sms;
+  const long long ctas = whole ? units : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
+  if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+  const size_t smem = (size_t)WARPS * kDecStages * DecBytes<FMT, D>::kStage + (size_t)WARPS * ROWS * (D + 4 + 3) * sizeof(float);
+  cudaError_t e = cudaFuncSetAttribute(decode_mx_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  if (e != cudaSuccess) return e;
+  e = launch_kernel("decode_mx", decode_mx_kernel<FMT, D, NT>, dim3((unsigned)ctas), dim3(32 * WARPS), smem, st, 1, chained, P, work, (const __nv_bfloat16*)q,
+                    (const uint8_t*)k, (const uint8_t*)v, k_idx, (__nv_bfloat16*)out, lse, parts, whole ? 1 : 0);
+  if (e != cudaSuccess) return e;
+  count_launch();
+  if (!whole) {
+    e = launch_kernel("decode_mx_join", decode_mx_join_kernel<D, NT>, dim3((unsigned)units, ROWS / 4), dim3(128), 0, st, 1, true, P, work, (const float*)parts, (int)ctas,
+                      (__nv_bfloat16*)out, lse);
+    if (e != cudaSuccess) return e;
+    count_launch();
+  }
+  return cudaGetLastError();
+}
+
+cudaError_t launch_decode_mx(const DevParams& P, int fmt, const void* q, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt, void* out,
+                             float* lse, float* parts, cudaStream_t st, bool chained) {
+  const bool one = dec_tiles(P) == 1;
+  return mx_dispatch(QUOKA_BF16, fmt, P.d, [&](auto, auto f, auto d) {
+    constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
+    return one ? launch_decode_mx_t<FMT, D, 1>(P, q, k, v, k_idx, k_cnt, out, lse, parts, st, chained)
+               : launch_decode_mx_t<FMT, D, 2>(P, q, k, v, k_idx, k_cnt, out, lse, parts, st, chained);
+  });
+}
+
+}  // namespace quoka

@@ -1,4 +1,6 @@
 // C entry points of the microscaled cache: validation, workspace, launch sequencing.
+#include <algorithm>
+
 #include "api_host.cuh"
 #include "mx.cuh"
 #include "mx_host.cuh"
@@ -36,6 +38,10 @@ static quoka_status run_score_keys_mx(const quoka_params* p, const quoka_mx_cach
 static quoka_status run_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const DevParams& P, const void* q, const void* k, const void* v,
                                 const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, const AttnPlan& plan,
                                 bool after_selection = false) {
+  if (p->impl == QUOKA_IMPL_AUTO && attn_mx_tc_supported(p) && decode_mx_applies(p)) {
+    QUOKA_TRY_CUDA(launch_decode_mx(P, mx->format, q, k, v, k_idx, k_cnt, out, lse, P.attn_partials, st, after_selection));
+    return QUOKA_OK;
+  }
   if (p->impl != QUOKA_IMPL_SIMT && attn_mx_tc_supported(p))
     return launch_attn_mx_tc(p, P, mx->format, q, k, v, k_idx, k_cnt, out, lse, st, after_selection, plan);
   if (p->impl == QUOKA_IMPL_TENSOR) return QUOKA_ERR_UNSUPPORTED;
@@ -43,7 +49,20 @@ static quoka_status run_attn_mx(const quoka_params* p, const quoka_mx_cache* mx,
   return QUOKA_OK;
 }
 
-static quoka_status check_ws_mx(const quoka_params* p, void* ws, size_t ws_bytes) { return check_ws(p, ws, ws_bytes); }
+// The scratch of a few query rows' attention comes last and has to be there.
+static size_t scratch_mx(const quoka_params* p) { return p->dtype == QUOKA_BF16 && decode_mx_applies(p) ? decode_mx_scratch_bytes(p) : 0; }
+static quoka_status check_ws_mx(const quoka_params* p, void* ws, size_t ws_bytes) {
+  const quoka_status st = check_ws(p, ws, ws_bytes);
+  if (st != QUOKA_OK) return st;
+  return ws_bytes < workspace_bytes_unsplit(p) + scratch_mx(p) ? QUOKA_ERR_WORKSPACE : QUOKA_OK;
+}
+// The buffers of an attention call that follows `plan`.
+static Workspace carve_mx(const quoka_params* p, void* ws, size_t ws_bytes, const AttnPlan& plan) {
+  if (scratch_mx(p) == 0) return carve(p, ws, ws_bytes, &plan);
+  Workspace w = carve(p, ws);
+  w.attn_partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + w.total);
+  return w;
+}
 
 }  // namespace quoka
 
@@ -55,7 +74,11 @@ quoka_status quoka_workspace_size_mx(const quoka_params* p, const quoka_mx_cache
   if (!bytes) return QUOKA_ERR_INVALID_ARG;
   const quoka_status st = validate_mx(p, mx);
   if (st != QUOKA_OK) return st;
-  return quoka_workspace_size(p, bytes);
+  size_t attn = 0;
+  if (quoka_workspace_size(p, &attn) != QUOKA_OK) return QUOKA_ERR_INVALID_ARG;
+  // (with the scratch of the shortest chunks, whatever this one's length: the last chunk of a prompt comes with the workspace of its longest)
+  *bytes = std::max(attn, workspace_bytes_unsplit(p) + (p->dtype == QUOKA_BF16 ? decode_mx_scratch_bytes(p) : 0));
+  return QUOKA_OK;
 }
 
 quoka_status quoka_append_kv_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* k_new, const void* v_new, void* k_cache,
@@ -102,7 +125,7 @@ quoka_status quoka_sparse_attn_mx(const quoka_params* p, const quoka_mx_cache* m
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws, ws_bytes, &plan)), q, k_cache, v_cache, k_idx, k_cnt, out, lse,
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve_mx(p, ws, ws_bytes, plan)), q, k_cache, v_cache, k_idx, k_cnt, out, lse,
                      static_cast<cudaStream_t>(stream), plan);
 }
 
@@ -114,7 +137,7 @@ quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cac
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   const AttnPlan plan = attn_plan_dense(p, attn_room(p, ws_bytes));
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve(p, ws, ws_bytes, &plan)), q, k_cache, v_cache, nullptr, nullptr, out, lse,
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve_mx(p, ws, ws_bytes, plan)), q, k_cache, v_cache, nullptr, nullptr, out, lse,
                      static_cast<cudaStream_t>(stream), plan);
 }
 
@@ -127,7 +150,7 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
-  const Workspace w = carve(p, ws, ws_bytes, &plan);
+  const Workspace w = carve_mx(p, ws, ws_bytes, plan);
   const DevParams P = make_dev_mx(p, mx, ws, w);
   int32_t* k_idx = k_idx_out ? k_idx_out : w.k_idx;
   int32_t* k_cnt = k_cnt_out ? k_cnt_out : w.k_cnt;

@@ -14,6 +14,7 @@ namespace quoka {
 
 constexpr int kMxShift = 16;                         // tiles hold values times 2^-kMxShift
 constexpr float kMxUnshift = 65536.f;
+constexpr int kNoNan = 0x7FFFFFFF;                   // no position, or key, that sees a value that is not finite
 
 // 16 elements of a row.
 template <int FMT> struct MxUnit;
@@ -34,6 +35,22 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // shifts and masks alone: 0 2 1 3 4 6 5 7, or 0 4 1 5 2 6 3 7 (mx_place).  Queries are put in the same order once per CTA, so that products
 // are the same; the columns of O come out in it, and the epilogues take them from there.  Against the plain order, by byte
 // permutations, it saves a third of the conversion's instructions on the integer pipe, which the softmax warps need too.
+// A word of elements in that order: two pairs of MXFP8, four of MXFP4.
+template <int FMT, int N>
+__device__ __forceinline__ void mx_to_pairs(uint32_t w, uint32_t factor2, uint32_t (&o)[N]) {
+  static_assert(N == (FMT == QUOKA_KV_MXFP8 ? 2 : 4), "pairs of a word");
+  if constexpr (FMT == QUOKA_KV_MXFP8) {
+    o[0] = (w << 8 & 0x80008000u) | (w << 4 & 0x07F007F0u);
+    o[1] = (w & 0x80008000u) | (w >> 4 & 0x07F007F0u);
+  } else {
+    o[0] = (w << 12 & 0x80008000u) | (w << 6 & 0x01C001C0u);
+    o[1] = (w << 8 & 0x80008000u) | (w << 2 & 0x01C001C0u);
+    o[2] = (w << 4 & 0x80008000u) | (w >> 2 & 0x01C001C0u);
+    o[3] = (w & 0x80008000u) | (w >> 6 & 0x01C001C0u);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = mul_bf16x2(o[i], factor2);
+}
 // PLAIN: in the plain order.
 template <int FMT, bool PLAIN = false>
 __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t factor2) {
@@ -48,24 +65,27 @@ __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t
       o[2] = __byte_perm(lo, w0, 0x6622); o[3] = __byte_perm(lo, w0, 0x7733);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)                        // (what stands below an element's bits is masked off)
+    for (int i = 0; i < 4; ++i) {                      // (what stands below an element's bits is masked off)
       o[i] = (o[i] & 0x80008000u) | (FMT == QUOKA_KV_MXFP8 ? o[i] >> 4 & 0x07F007F0u : o[i] >> 6 & 0x01C001C0u);
+      o[i] = mul_bf16x2(o[i], factor2);
+    }
   } else if constexpr (FMT == QUOKA_KV_MXFP8) {
-    o[0] = (w0 << 8 & 0x80008000u) | (w0 << 4 & 0x07F007F0u);
-    o[1] = (w0 & 0x80008000u) | (w0 >> 4 & 0x07F007F0u);
-    o[2] = (w1 << 8 & 0x80008000u) | (w1 << 4 & 0x07F007F0u);
-    o[3] = (w1 & 0x80008000u) | (w1 >> 4 & 0x07F007F0u);
+    uint32_t a[2], b[2];
+    mx_to_pairs<FMT>(w0, factor2, a);
+    mx_to_pairs<FMT>(w1, factor2, b);
+    o[0] = a[0]; o[1] = a[1]; o[2] = b[0]; o[3] = b[1];
   } else {
-    o[0] = (w0 << 12 & 0x80008000u) | (w0 << 6 & 0x01C001C0u);
-    o[1] = (w0 << 8 & 0x80008000u) | (w0 << 2 & 0x01C001C0u);
-    o[2] = (w0 << 4 & 0x80008000u) | (w0 >> 2 & 0x01C001C0u);
-    o[3] = (w0 & 0x80008000u) | (w0 >> 6 & 0x01C001C0u);
+    mx_to_pairs<FMT>(w0, factor2, o);
   }
-#pragma unroll
-  for (int i = 0; i < 4; ++i) o[i] = mul_bf16x2(o[i], factor2);
   return make_uint4(o[0], o[1], o[2], o[3]);
 }
 
+// 8 bf16 numbers in plain order, put in that order.
+template <int FMT>
+__device__ __forceinline__ uint4 mx_order(uint4 w) {
+  const uint32_t a = FMT == QUOKA_KV_MXFP8 ? w.y : w.z, b = FMT == QUOKA_KV_MXFP8 ? w.z : w.y;     // what goes with x, and with w
+  return make_uint4(__byte_perm(w.x, a, 0x5410), __byte_perm(w.x, a, 0x7632), __byte_perm(b, w.w, 0x5410), __byte_perm(b, w.w, 0x7632));
+}
 // An item is ROWS cache rows, COLS columns of each: raw in a stage of shared memory, [ROWS][COLS * bits / 8 bytes] and a word of
 // scale bytes per row, then bf16 in a tile, [64-column halves][ROWS][128 B] with 16-byte pieces swizzled by row.  What fills stages (the
 // copy engine where rows follow one another, else cp.async) and what converts them are different warps: each of the two alone, one
