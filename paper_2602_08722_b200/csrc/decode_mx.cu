@@ -64,33 +64,57 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   return r;
 }
 
-// The list of granules: unit = (sequence, KV head, row group), in this order.
+// The list of granules: unit = (sequence, KV head, row group), in this order.  CTA i has granules [i share, (i + 1) share), share the
+// smallest that reaches.
 struct DecWork {
   int groups;              // row groups of a KV head
   const int32_t* k_cnt;    // listed: rows in the list (device), or null
-  // keys of a sequence: cached (listed or all), then the chunk's own
-  __device__ __forceinline__ int cached(const DevParams& P, int s) const { return k_cnt ? __ldcg(k_cnt + s) : load_input<true>(P.ctx_len + s); }
-  __device__ __forceinline__ int granules(const DevParams& P, int s) const { return (cached(P, s) + P.chunk + kDecGranule - 1) / kDecGranule; }
-  // granules of sequences [0, s), s <= batch (whole warp)
-  __device__ __forceinline__ long long before(const DevParams& P, int s, int lane) const {
-    long long sum = 0;
-    for (int s0 = 0; s0 < s; s0 += 32) sum += __reduce_add_sync(0xFFFFFFFFu, s0 + lane < s ? granules(P, s0 + lane) : 0);
-    return sum * (P.n_kv * groups);
+};
+// A sequence's lengths: cached keys attended to (listed or all), cached rows.
+struct DecLens {
+  int cnt, T;
+  __device__ __forceinline__ DecLens(const DevParams& P, const DecWork& w, int s) : T(load_input<true>(P.ctx_len + s)) { cnt = w.k_cnt ? __ldcg(w.k_cnt + s) : T; }
+  __device__ __forceinline__ DecLens(int cnt_, int T_) : cnt(cnt_), T(T_) {}
+  __device__ __forceinline__ int granules(const DevParams& P) const { return (cnt + P.chunk + kDecGranule - 1) / kDecGranule; }
+};
+// Granules of the whole list and of the sequences before s (whole warp; one round trip for up to 32 sequences).
+struct DecTotals {
+  DecLens lane_lens;       // this lane's sequence of the first 32
+  long long total, before;
+  __device__ __forceinline__ DecTotals(const DevParams& P, const DecWork& w, int s, int lane) : lane_lens(0, 0), total(0), before(0) {
+    for (int s0 = 0; s0 < P.batch; s0 += 32) {
+      const bool there = s0 + lane < P.batch;
+      const DecLens mine = there ? DecLens(P, w, s0 + lane) : DecLens(0, 0);
+      if (s0 == 0) lane_lens = mine;
+      const int n = there ? mine.granules(P) : 0;
+      total += __reduce_add_sync(0xFFFFFFFFu, n);
+      before += __reduce_add_sync(0xFFFFFFFFu, s0 + lane < s ? n : 0);
+    }
+    total *= P.n_kv * w.groups;
+    before *= P.n_kv * w.groups;
+  }
+  __device__ __forceinline__ long long share(int ctas) const {
+    return total < 0x7FFFFFFF ? (long long)(((uint32_t)total + (uint32_t)ctas - 1) / (uint32_t)ctas) : (total + ctas - 1) / ctas;
   }
 };
+__device__ __forceinline__ int dec_div(long long a, long long b) {      // both small, as a rule
+  return (a | b) >> 31 == 0 ? (int)((uint32_t)a / (uint32_t)b) : (int)(a / b);
+}
 // A CTA's share of the list, part of a unit after part of a unit; identical in every warp.
 struct DecPart {
   int s, kv, grp;          // unit
-  int cnt, n;              // its cached keys and its granules
+  DecLens lens;
+  int n;                   // its granules
   int begin, end;          // granules of this part
   long long left;          // granules of the share behind this part
-  __device__ __forceinline__ void seek(const DevParams& P, const DecWork& w, long long lo, long long hi, int lane) {
-    left = hi - lo;
-    s = 0;
+  // the share [lo, hi)
+  __device__ __forceinline__ DecPart(const DevParams& P, const DecWork& w, const DecTotals& all, long long lo, long long hi, int lane)
+      : lens(all.lane_lens), left(hi - lo) {
     const int heads = P.n_kv * w.groups;
-    for (;; s += 32) {                                // the sequence that lo is in
-      const long long mine = s + lane < P.batch ? (long long)w.granules(P, s + lane) * heads : 0;
-      long long incl = mine;
+    for (s = 0;; s += 32) {                           // the sequence that lo is in
+      const DecLens mine = s == 0 ? all.lane_lens : s + lane < P.batch ? DecLens(P, w, s + lane) : DecLens(0, 0);
+      const long long here = s + lane < P.batch ? (long long)mine.granules(P) * heads : 0;
+      long long incl = here;
 #pragma unroll
       for (int o = 1; o < 32; o <<= 1) {
         const long long v = __shfl_up_sync(0xFFFFFFFFu, incl, o);
@@ -99,22 +123,24 @@ struct DecPart {
       const uint32_t hit = __ballot_sync(0xFFFFFFFFu, incl > lo);
       if (hit != 0) {
         const int src = __ffs(hit) - 1;
-        lo -= __shfl_sync(0xFFFFFFFFu, incl - mine, src);
+        lo -= __shfl_sync(0xFFFFFFFFu, incl - here, src);
+        lens = DecLens(__shfl_sync(0xFFFFFFFFu, mine.cnt, src), __shfl_sync(0xFFFFFFFFu, mine.T, src));
         s += src;
         break;
       }
       lo -= __shfl_sync(0xFFFFFFFFu, incl, 31);
     }
-    set(P, w);
-    const int unit = (int)(lo / n);
+    n = lens.granules(P);
+    const int unit = dec_div(lo, n);
     kv = unit / w.groups;
     grp = unit % w.groups;
-    begin = (int)(lo % n);
+    begin = (int)(lo - (long long)unit * n);
     cut();
   }
-  __device__ __forceinline__ void set(const DevParams& P, const DecWork& w) {
-    cnt = w.cached(P, s);
-    n = (cnt + P.chunk + kDecGranule - 1) / kDecGranule;
+  // one whole unit
+  __device__ __forceinline__ DecPart(const DevParams& P, const DecWork& w, int unit)
+      : s(unit / (P.n_kv * w.groups)), kv(unit / w.groups % P.n_kv), grp(unit % w.groups), lens(P, w, unit / (P.n_kv * w.groups)), begin(0), left(0) {
+    n = end = lens.granules(P);
   }
   __device__ __forceinline__ void cut() {
     end = (int)min((long long)n, begin + left);
@@ -125,7 +151,11 @@ struct DecPart {
     if (left <= 0) { begin = end; return false; }
     if (++grp == w.groups) {
       grp = 0;
-      if (++kv == P.n_kv) { kv = 0; ++s; set(P, w); }
+      if (++kv == P.n_kv) {
+        kv = 0;
+        lens = DecLens(P, w, ++s);
+        n = lens.granules(P);
+      }
     }
     begin = 0;
     cut();
@@ -149,20 +179,15 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   float* merge = reinterpret_cast<float*>(dec_smem + (size_t)WARPS * ST * B::kStage);        // [WARPS][ROWS][LD], then m, l, lx [WARPS][ROWS]
   float* merge_ml = merge + WARPS * ROWS * LD;
   // ---- this CTA's share
-  long long lo, hi;
-  if (whole_units) {                                  // one unit per CTA
-    const int unit = blockIdx.x, per_s = P.n_kv * work.groups, s = unit / per_s;
-    const int n = work.granules(P, s);
-    lo = work.before(P, s, lane) + (long long)(unit % per_s) * n;
-    hi = lo + n;
-  } else {
-    const long long total = work.before(P, P.batch, lane);
-    lo = total * blockIdx.x / gridDim.x;
-    hi = total * (blockIdx.x + 1) / gridDim.x;
-  }
-  if (lo >= hi) return;
-  DecPart in;
-  in.seek(P, work, lo, hi, lane);
+  const auto share = [&]() -> DecPart {
+    if (whole_units) return DecPart(P, work, blockIdx.x);
+    const DecTotals all(P, work, 0, lane);
+    const long long each = all.share(gridDim.x), lo = min(each * blockIdx.x, all.total);
+    if (lo == all.total) { DecPart none(P, work, 0); none.end = 0; return none; }
+    return DecPart(P, work, all, lo, min(lo + each, all.total), lane);
+  };
+  DecPart in = share();
+  if (in.begin >= in.end) return;                     // (nothing of the list is left for this CTA)
   DecPart part = in;
   // ---- copies: granules begin + warp, + WARPS .. of every part.  Lanes 0-15 look after a row's keys, 16-31 after its values: row numbers
   // two granules ahead, places one ahead.
@@ -173,8 +198,8 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   const auto row_number = [&]() -> int {              // of this lane's row in granule pos, -1: none
     if (!more) return -1;
     const int u = pos * kDecGranule + (lane & 15);
-    if (u >= in.cnt + P.chunk) return -1;
-    if (u >= in.cnt) return load_input<true>(P.ctx_len + in.s) + (u - in.cnt);
+    if (u >= in.lens.cnt + P.chunk) return -1;
+    if (u >= in.lens.cnt) return in.lens.T + (u - in.lens.cnt);
     return k_idx ? __ldcg(k_idx + ((long long)in.s * P.n_kv + in.kv) * P.budget_cap + u) : u;
   };
   int t_next, s_next = 0, kv_next = 0;                // of the granule whose places are worked out next
@@ -267,8 +292,8 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-      for (int e = 0; e < 2; ++e) sees[nt][e] = part.cnt + min(first_row + 8 * nt + 2 * c + e, P.chunk * P.group - 1) / P.group + 1;
-    const int all_see = part.cnt + first_row / P.group + 1;         // keys that every row sees
+      for (int e = 0; e < 2; ++e) sees[nt][e] = part.lens.cnt + min(first_row + 8 * nt + 2 * c + e, P.chunk * P.group - 1) / P.group + 1;
+    const int all_see = part.lens.cnt + first_row / P.group + 1;         // keys that every row sees
 #pragma unroll 1
     for (int gr = part.begin + warp; gr < part.end; gr += WARPS) {
       cp_async_wait<ST - 1>();
@@ -467,52 +492,70 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   cp_async_wait_all();                                 // nothing of this thread is in flight at exit
 }
 
-// Units that several CTAs of the list share, a warp per query row: the parts added up in their order.
+// Units that several CTAs of the list share, a CTA per query row: its warps take parts in turn, all loads of a warp's parts at once as a rule
+// (a loop over the parts by one warp took 15 us for 20 of them), and add them up in a fixed order.
+constexpr int kJoinWarps = 4, kJoinAtOnce = 6;
 template <int D, int NT>
-__global__ void __launch_bounds__(128) decode_mx_join_kernel(DevParams P, DecWork work, const float* __restrict__ parts, int ctas, __nv_bfloat16* __restrict__ out,
-                                                             float* __restrict__ lse) {
+__global__ void __launch_bounds__(32 * kJoinWarps) decode_mx_join_kernel(DevParams P, DecWork work, const float* __restrict__ parts, int ctas,
+                                                                         __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
   constexpr int ROWS = 8 * NT, PER = D / 32;
+  __shared__ float sm[kJoinWarps][3], so[kJoinWarps][D];
   grid_dependency_wait();
   grid_launch_dependents();
-  const int lane = threadIdx.x & 31, unit = blockIdx.x, per_s = P.n_kv * work.groups, s = unit / per_s;
-  const int row = blockIdx.y * 4 + (threadIdx.x >> 5), grp = unit % work.groups, r = grp * ROWS + row;
-  const int n = work.granules(P, s);
-  const long long total = work.before(P, P.batch, lane), a = work.before(P, s, lane) + (long long)(unit % per_s) * n, b = a + n;
-  if (row >= ROWS || r >= P.chunk * P.group) return;
-  // CTA i has [total i / ctas, total (i + 1) / ctas)
-  const auto cta_of = [&](long long at) {
-    long long i = at * ctas / total;
-    while (total * (i + 1) / ctas <= at) ++i;
-    while (total * i / ctas > at) --i;
-    return (int)i;
-  };
-  const int first = cta_of(a), last = cta_of(b - 1);
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, unit = blockIdx.x, per_s = P.n_kv * work.groups, s = unit / per_s;
+  const int row = blockIdx.y, r = unit % work.groups * ROWS + row;
+  if (r >= P.chunk * P.group) return;
+  const DecTotals all(P, work, s, lane);
+  const int n = DecLens(P, work, s).granules(P);
+  const long long each = all.share(ctas), a = all.before + (long long)(unit % per_s) * n;
+  const int first = dec_div(a, each), last = dec_div(a + n - 1, each);
   if (first == last) return;                           // (written by that CTA)
   const auto slot = [&](int i) { return parts + (size_t)(2 * i + (i == first ? 1 : 0)) * ROWS * (D + 3); };
-  float mx = -INFINITY;
-  for (int i = first + lane; i <= last; i += 32) mx = fmaxf(mx, __ldcg(slot(i) + ROWS * D + row));
-#pragma unroll
-  for (int sh = 16; sh > 0; sh >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, sh));
-  float sum = 0.f, sumx = 0.f, acc[PER];
+  // weights of a reference point against another; what has seen nothing weighs nothing
+  const auto weight = [](float m, float mx) { return m == mx ? 1.f : m == -INFINITY ? 0.f : ex2(m - mx); };
+  float mx = -INFINITY, sum = 0.f, sumx = 0.f, acc[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) acc[e] = 0.f;
-#pragma unroll 4
-  for (int i = first; i <= last; ++i) {
-    const float* p = slot(i);
-    const float mi = __ldcg(p + ROWS * D + row), wt = mi == -INFINITY && mx != -INFINITY ? 0.f : mi == mx ? 1.f : ex2(mi - mx);
-    sum = fmaf(wt, __ldcg(p + ROWS * (D + 1) + row), sum);
-    sumx = fmaf(wt, __ldcg(p + ROWS * (D + 2) + row), sumx);
-    float v[PER];
-    load_vec<float, PER, true>(p + row * D + lane * PER, v);
+  for (int i0 = first + warp; i0 <= last; i0 += kJoinWarps * kJoinAtOnce) {
+    float m[kJoinAtOnce], l[kJoinAtOnce], lx[kJoinAtOnce], v[kJoinAtOnce][PER];
 #pragma unroll
-    for (int e = 0; e < PER; ++e) acc[e] = fmaf(wt, v[e], acc[e]);
+    for (int j = 0; j < kJoinAtOnce; ++j) {
+      const float* p = slot(min(i0 + j * kJoinWarps, last));
+      m[j] = __ldcg(p + ROWS * D + row);
+      l[j] = __ldcg(p + ROWS * (D + 1) + row);
+      lx[j] = __ldcg(p + ROWS * (D + 2) + row);
+      load_vec<float, PER, true>(p + row * D + lane * PER, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < kJoinAtOnce; ++j)
+      if (i0 + j * kJoinWarps <= last) {
+        const float top = fmaxf(mx, m[j]), w0 = weight(mx, top), w1 = weight(m[j], top);
+        mx = top;
+        sum = fmaf(w1, l[j], sum * w0);
+        sumx = fmaf(w1, lx[j], sumx * w0);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) acc[e] = fmaf(w1, v[j][e], acc[e] * w0);
+      }
   }
-  const int h = unit % per_s / work.groups * P.group + r % P.group, pos = r / P.group;
-  const float inv = kMxUnshift / sum;
+  if (lane == 0) { sm[warp][0] = mx; sm[warp][1] = sum; sm[warp][2] = sumx; }
 #pragma unroll
-  for (int e = 0; e < PER; ++e) acc[e] *= inv;
-  store_vec<__nv_bfloat16, PER>(out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)pos * P.o_st + lane * PER, acc);
-  if (lse && lane == 0) lse[((long long)s * P.n_q + h) * P.chunk + pos] = (mx + log2f(sumx)) * 0.6931471805599453f;
+  for (int e = 0; e < PER; ++e) so[warp][lane * PER + e] = acc[e];
+  __syncthreads();
+  const int h = unit % per_s / work.groups * P.group + r % P.group, pos = r / P.group;
+  for (int col = threadIdx.x; col < D; col += 32 * kJoinWarps) {
+    float top = sm[0][0], total = 0.f, totalx = 0.f, o = 0.f;
+#pragma unroll
+    for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, sm[w][0]);
+#pragma unroll
+    for (int w = 0; w < kJoinWarps; ++w) {
+      const float wt = weight(sm[w][0], top);
+      total = fmaf(wt, sm[w][1], total);
+      totalx = fmaf(wt, sm[w][2], totalx);
+      o = fmaf(wt, so[w][col], o);
+    }
+    out[(long long)s * P.o_sb + (long long)h * P.o_sh + (long long)pos * P.o_st + col] = __float2bfloat16_rn(o * (kMxUnshift / total));
+    if (lse && col == 0) lse[((long long)s * P.n_q + h) * P.chunk + pos] = (top + log2f(totalx)) * 0.6931471805599453f;
+  }
 }
 
 // ---------------------------------------------------------------------------------------------- host
@@ -551,7 +594,7 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   if (e != cudaSuccess) return e;
   count_launch();
   if (!whole) {
-    e = launch_kernel("decode_mx_join", decode_mx_join_kernel<D, NT>, dim3((unsigned)units, ROWS / 4), dim3(128), 0, st, 1, true, P, work, (const float*)parts, (int)ctas,
+    e = launch_kernel("decode_mx_join", decode_mx_join_kernel<D, NT>, dim3((unsigned)units, ROWS), dim3(32 * kJoinWarps), 0, st, 1, true, P, work, (const float*)parts, (int)ctas,
                       (__nv_bfloat16*)out, lse);
     if (e != cudaSuccess) return e;
     count_launch();
