@@ -5,15 +5,26 @@
 // that turn 8 or 4 bits into operands.  So the products are matrix instructions with the keys on the M side (m16n8k16: the query
 // rows fill the 8 columns, a 128-row tcgen05 tile would have 4 or 8 rows of use in 128), whose operands a lane builds in registers from the
 // bytes it copied itself:
-//   S^T = K Q^T   a lane brings 16-byte pieces of two key rows; which columns they are does not matter to the sum, Q's fragment has the same
-//   O^T = V^T P^T a lane brings the same 8 or 16 columns of four value rows and interleaves the rows of a pair
-// P^T comes out of S^T by an 8 x 8 transposition (movmatrix).  Nothing but the scale words crosses lanes on the way in.
+//   S^T = K Q^T   a lane brings 16-byte pieces of key rows; which columns they are does not matter to the sum, Q's fragment has the same
+//   O^T = V^T P^T a lane brings the same 8 or 16 columns of value rows and interleaves the rows of a pair
+// P^T comes out of S^T by 8 x 8 transpositions (movmatrix).  Nothing but the scale words crosses lanes on the way in.
 //
-// Split: the 16-key granules of all (sequence, KV head, row group) in one list, cut into equal contiguous shares, one per CTA; inside a
+// The operands are fp16, which the conversion instructions make of 8 and 4 bits at once (by shifts and masks, as bf16, it took twice
+// the instructions: 637 for 16 keys of 128 columns, 171 us for a step of 16 sequences of 8K to 32K rows).  Its range does not limit:
+//   K  each row is scaled by its largest block's exponent, which goes into the row's score in fp32;
+//   Q  each row by a power of two to 2^14 .. 2^15, taken off the score in fp32 (bf16 has 8 bits: nothing is lost but what is 2^-39 of the
+//      row's largest element);
+//   V  by the largest exponent a lane has met in its columns, to which O is rescaled if one 2^7 times that comes (rare);
+//   P  weights 2^(x - m), m a reference point that the largest exponent x exceeds by 7 when it is set and by 15 at most: weights below 2^-25, against a largest one of
+//      2^7 or more, vanish (a hundred thousand of them are 2^-15 of the sum).
+//
+// Split: the 32-key granules of all (sequence, KV head, row group) in one list, cut into equal contiguous shares, one per CTA; inside a
 // CTA the warps take granules in turn, each with a running maximum, sum and output of its own, added up at the end of a unit's part.
 // A unit that several CTAs share is added up by a second kernel, part by part in order.  Long lists are balanced whatever the
-// sequences' lengths are.  Weights are rounded to bf16 for the product and divided by their sum as rounded, so that they add up to
+// sequences' lengths are.  Weights are rounded to fp16 for the product and divided by their sum as rounded, so that they add up to
 // one; the log-sum-exp is that of the weights before.
+#include <cuda_fp16.h>
+
 #include <algorithm>
 
 #include "mx_host.cuh"
@@ -24,18 +35,18 @@ namespace quoka {
 
 using namespace ptx;
 
-constexpr int kDecGranule = 16;
+constexpr int kDecGranule = 32;
+constexpr int kDecWarps = 8;
+constexpr int kDecStages = 2;
 
-template <int NT> constexpr int kDecWarps = NT == 1 ? 12 : 8;
-constexpr int kDecStages = 3;
-
-// What a lane copies of a granule: K_PIECES pieces of K_BYTES of each of two rows, V_BYTES of each of four.
+// What a lane copies of a granule: kKPieces pieces of kKBytes of each of four key rows, kVBytes of each of eight value rows.
 template <int FMT, int D>
 struct DecBytes {
   static constexpr int kRow = D * kMxBits<FMT> / 8;
   static constexpr int kKPieces = kRow == 128 ? 2 : 1, kKBytes = kRow / 4 / kKPieces, kVBytes = kRow / 8;
-  static constexpr uint32_t kK = 2 * kKPieces * 32 * kKBytes, kV = 4 * 32 * kVBytes;
-  static constexpr uint32_t kStage = kK + kV + (D == 128 ? 128 : 256);       // scale words of 16 rows of K and of V, head_dim 64 also their shifts
+  static constexpr uint32_t kK = 4 * kKPieces * 32 * kKBytes, kV = 8 * 32 * kVBytes;
+  static constexpr uint32_t kMeta = D == 128 ? 256 : 384;      // scale words of the rows' keys, of their values, head_dim 64 also their shifts
+  static constexpr uint32_t kStage = kK + kV + kMeta;
   static_assert(kK == kDecGranule * kRow && kV == kDecGranule * kRow, "a granule");
 };
 
@@ -54,10 +65,38 @@ __device__ __forceinline__ void lds_words(uint32_t at, uint32_t* w) {
   else if constexpr (WORDS == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
   else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at) : "memory");
 }
-__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t f16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+  uint32_t d;
+  asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+// A word of elements as fp16 pairs in order: two of MXFP8, four of MXFP4 (a byte has a pair).
+template <int FMT, int N>
+__device__ __forceinline__ void f16_pairs(uint32_t w, uint32_t factor2, uint32_t (&o)[N]) {
+  static_assert(N == (FMT == QUOKA_KV_MXFP8 ? 2 : 4), "pairs of a word");
+  if constexpr (FMT == QUOKA_KV_MXFP8) {
+    asm("{\n\t.reg .b16 a, b;\n\tmov.b32 {a, b}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, a;\n\tcvt.rn.f16x2.e4m3x2 %1, b;\n\t}" : "=r"(o[0]), "=r"(o[1]) : "r"(w));
+  } else {
+    asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %4;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, c;\n\tcvt.rn.f16x2.e2m1x2 %3, d;\n\t}" : "=r"(o[0]), "=r"(o[1]), "=r"(o[2]), "=r"(o[3]) : "r"(w));
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = mul_f16x2(o[i], factor2);
+}
+// 2^diff, diff <= 15, as an fp16 number (zero below its range).
+__device__ __forceinline__ float pow2_at_most_15(int diff) { return __uint_as_float((uint32_t)(max(diff, -60) + 127) << 23); }
+constexpr int kDecMaxAbove = 15, kDecHeadroom = 7;       // of a weight's exponent over the reference point, at most and when it is set
+constexpr int kDecScaleAbove = 7;                        // of a value block's exponent over O's: 448 * 2^7 is an fp16 number
+
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
@@ -164,11 +203,11 @@ struct DecPart {
 };
 
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(32 * kDecWarps<NT>, 1)
+__global__ void __launch_bounds__(32 * kDecWarps, 1)
 decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                  const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units) {
   typedef DecBytes<FMT, D> B;
-  constexpr int WARPS = kDecWarps<NT>, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
+  constexpr int WARPS = kDecWarps, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
   constexpr int KW = B::kKBytes * B::kKPieces / 4, VW = B::kVBytes / 4;      // words of a lane per row
   constexpr int LD = D + 4;                                                  // floats of a row of the merge buffer
   extern __shared__ __align__(16) unsigned char dec_smem[];
@@ -189,49 +228,51 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   DecPart in = share();
   if (in.begin >= in.end) return;                     // (nothing of the list is left for this CTA)
   DecPart part = in;
-  // ---- copies: granules begin + warp, + WARPS .. of every part.  Lanes 0-15 look after a row's keys, 16-31 after its values: row numbers
-  // two granules ahead, places one ahead.
+  // ---- copies: granules begin + warp, + WARPS .. of every part.  A lane looks after a row: its number two granules ahead, its place one.
   MxPlaces places(P);
   int pos = in.begin + warp;
   bool more = true;
-  const auto settle = [&]() { while (more && pos >= in.end) { more = in.next(P, work); pos = in.begin + warp; } };
-  const auto row_number = [&]() -> int {              // of this lane's row in granule pos, -1: none
-    if (!more) return -1;
-    const int u = pos * kDecGranule + (lane & 15);
-    if (u >= in.lens.cnt + P.chunk) return -1;
-    if (u >= in.lens.cnt) return in.lens.T + (u - in.lens.cnt);
-    return k_idx ? __ldcg(k_idx + ((long long)in.s * P.n_kv + in.kv) * P.budget_cap + u) : u;
-  };
-  int t_next, s_next = 0, kv_next = 0;                // of the granule whose places are worked out next
+  int n_next, s_next = 0, kv_next = 0;                // of the granule whose places are worked out next
   bool live_next = false;
   uint32_t place = kNoRow, srow = 0;                  // of the granule that is copied next
   bool live = false;
   const auto ask = [&]() {
-    settle();
+    while (more && pos >= in.end) { more = in.next(P, work); pos = in.begin + warp; }
     live_next = more;
     s_next = in.s; kv_next = in.kv;
-    t_next = row_number();
+    n_next = -1;
+    if (more) {
+      const int u = pos * kDecGranule + lane;
+      if (u < in.lens.cnt) n_next = k_idx ? __ldcg(k_idx + ((long long)in.s * P.n_kv + in.kv) * P.budget_cap + u) : u;
+      else if (u < in.lens.cnt + P.chunk) n_next = in.lens.T + (u - in.lens.cnt);
+    }
     pos += WARPS;
   };
+  int s_at = -1, kv_at = -1;
   const auto locate = [&]() {
     live = live_next;
-    int t = t_next;
+    if (!live) return;
+    int t = n_next;
 #ifdef QUOKA_DEBUG
-    if (live && (t < -1 || t >= __ldg(P.ctx_len + s_next) + P.chunk)) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
+    if (t < -1 || t >= __ldg(P.ctx_len + s_next) + P.chunk) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
 #endif
-    places.at_head(P, s_next, kv_next);
-    places.of(P, live ? t : -1, place, srow);
+    if (s_next != s_at || kv_next != kv_at) { places.at_head(P, s_next, kv_next); s_at = s_next; kv_at = kv_next; }
+    places.of(P, t, place, srow);
   };
   const auto fill = [&](int stage) {
     if (live) {
       const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV + 4 * lane;
-      const uint8_t* sc = lane < 16 ? P.k_scale : P.v_scale;
-      if (place != kNoRow) cp_async_4(meta, sc + (D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4));
-      else asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta), "r"(0u) : "memory");
-      if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 128), "r"((srow & 1u) * 16) : "memory");
+      if (place != kNoRow) {
+        const size_t word = D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4;
+        cp_async_4(meta, P.k_scale + word);
+        cp_async_4(meta + 128, P.v_scale + word);
+      } else {
+        asm volatile("st.shared.u32 [%0], %2;\n\tst.shared.u32 [%1], %2;" ::"r"(meta), "r"(meta + 128), "r"(0u) : "memory");
+      }
+      if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 256), "r"((srow & 1u) * 16) : "memory");
       constexpr int kUnit = 2 * kMxBits<FMT>;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < 4; ++i) {
         const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, g + 8 * i);
         const uint8_t* src = kc + (size_t)(row == kNoRow ? 0u : row) * kUnit + c * B::kKBytes;
 #pragma unroll
@@ -239,7 +280,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
           cp_async_n<B::kKBytes>(at + (uint32_t)((i * B::kKPieces + p) * 32 + lane) * B::kKBytes, src + 64 * p, row != kNoRow);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < 8; ++i) {                    // keys 2 c, 2 c + 1, and 8 on, of both halves of the granule
         const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, 2 * c + (i & 1) + 8 * (i >> 1));
         cp_async_n<B::kVBytes>(at + B::kK + (uint32_t)(i * 32 + lane) * B::kVBytes, vc + (size_t)(row == kNoRow ? 0u : row) * kUnit + g * B::kVBytes, row != kNoRow);
       }
@@ -254,27 +295,42 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
   for (int i = 0; i < ST; ++i) fill(i);
 
-  const float scale_log2 = P.scale * 1.4426950408889634f * kMxUnshift;
   uint32_t qf[NT][2 * KSTEPS];
+  float qs[NT][2];                                    // to log2 units of the logits, of the rows of this lane's columns
   float o[NT][TILES][4], m[NT][2], l[NT][2], lx[NT][2];    // lx: the sum of the weights before they are rounded
   int stage = 0, s_cur = -1, kv_cur = -1, grp_cur = -1;
   for (bool again = true; again;) {
     const int first_row = part.grp * ROWS, n_rows = min(ROWS, P.chunk * P.group - first_row);
-    // ---- the part's query rows, in the order of the converted keys
+    // ---- the part's query rows
     if (part.s != s_cur || part.kv != kv_cur || part.grp != grp_cur) {
       s_cur = part.s; kv_cur = part.kv; grp_cur = part.grp;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int row = 8 * nt + g, r = first_row + row;
         const __nv_bfloat16* qr = q + (long long)part.s * P.q_sb + (long long)(part.kv * P.group + r % P.group) * P.q_sh + (long long)(r / P.group) * P.q_st;
+        uint4 w[D / 32];
+        uint32_t top = 0;                             // bits of the row's largest magnitude
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {             // 8 columns of the lane's D / 4
           const int col = FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j;
-          uint4 w = make_uint4(0, 0, 0, 0);
-          if (row < n_rows) w = load_input<true>(reinterpret_cast<const uint4*>(qr + col));
-          w = mx_order<FMT>(w);
-          qf[nt][4 * j] = w.x; qf[nt][4 * j + 1] = w.y; qf[nt][4 * j + 2] = w.z; qf[nt][4 * j + 3] = w.w;
+          w[j] = make_uint4(0, 0, 0, 0);
+          if (row < n_rows) w[j] = load_input<true>(reinterpret_cast<const uint4*>(qr + col));
+          const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max(top, max(x[i] << 16 & 0x7FFF0000u, x[i] & 0x7FFF0000u));
         }
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const int up = min(14 + 127 - (int)(top >> 23), 120);          // (an element that is not finite stays so)
+        const float f = __uint_as_float((uint32_t)(127 + up) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) {
+          const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) qf[nt][4 * j + i] = f16x2(__uint_as_float(x[i] << 16) * f, __uint_as_float(x[i] & 0xFFFF0000u) * f);
+        }
+#pragma unroll
+        for (int e = 0; e < 2; ++e) qs[nt][e] = __shfl_sync(0xFFFFFFFFu, back, 4 * (2 * c + e)) * (P.scale * 1.4426950408889634f);
       }
     }
 #pragma unroll
@@ -286,6 +342,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nt][t][e] = 0.f;
     }
+    int ov = 0;                                        // scale byte of O's columns in this lane (all of one block of 32)
     int nan_u = kNoNan;                                // first key, in the order of visibility, with a value that is not finite in this lane's columns
     // keys that the rows of this lane's columns see: 2 c and 2 c + 1 of each tile
     int sees[NT][2];
@@ -293,86 +350,96 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) sees[nt][e] = part.lens.cnt + min(first_row + 8 * nt + 2 * c + e, P.chunk * P.group - 1) / P.group + 1;
-    const int all_see = part.lens.cnt + first_row / P.group + 1;         // keys that every row sees
+    const int all_see = part.lens.cnt + first_row / P.group + 1;       // keys that every row sees
 #pragma unroll 1
     for (int gr = part.begin + warp; gr < part.end; gr += WARPS) {
       cp_async_wait<ST - 1>();
       __syncwarp();
       const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV;
-      const auto scale_word = [&](int i) {
+      // scale bytes of the i-th row's keys (0) or values (128)
+      const auto scale_word = [&](int what, int i) {
         uint32_t w;
-        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(meta + 4 * i) : "memory");
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(meta + what + 4 * i) : "memory");
         if (D == 64) {
           uint32_t shift;
-          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 128 + 4 * i) : "memory");
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 256 + 4 * i) : "memory");
           w = w >> shift & 0xFFFFu;
         }
         return w;
       };
-      // ---- S^T = K Q^T
-      float sc[NT][4];
+      // ---- S^T = K Q^T, 16 keys at a time
+      float sc[2][NT][4];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sc[nt][e] = 0.f;
-      {
-        uint32_t w0[KW], w1[KW];
-#pragma unroll
-        for (int p = 0; p < B::kKPieces; ++p) {
-          lds_words<B::kKBytes / 4>(at + (uint32_t)(p * 32 + lane) * B::kKBytes, w0 + p * (B::kKBytes / 4));
-          lds_words<B::kKBytes / 4>(at + (uint32_t)((B::kKPieces + p) * 32 + lane) * B::kKBytes, w1 + p * (B::kKBytes / 4));
-        }
-        const uint32_t sw0 = scale_word(g), sw1 = scale_word(g + 8);
-        // the lane's block(s): 32 columns from c * D / 4 on, two of 16 columns at 8 bits and head_dim 128
-        const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
-        const auto factor = [&](uint32_t word, int b) {
-          const uint32_t e = word >> (8 * b) & 0xFFu;
-          return e == kMxNanScale ? kBf16Nan2 : mx_factor2<FMT>(e);
-        };
-        uint32_t f0 = factor(sw0, blk), f1 = factor(sw1, blk);
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-          if (B::kKPieces == 2 && j == KW / 2) { f0 = factor(sw0, blk + 2); f1 = factor(sw1, blk + 2); }
-          if constexpr (FMT == QUOKA_KV_MXFP8) {
-            uint32_t a[2], b[2];
-            mx_to_pairs<FMT>(w0[j], f0, a);
-            mx_to_pairs<FMT>(w1[j], f1, b);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_bf16(sc[nt], a[0], b[0], a[1], b[1], qf[nt][2 * j], qf[nt][2 * j + 1]);
-          } else {
-            uint32_t a[4], b[4];
-            mx_to_pairs<FMT>(w0[j], f0, a);
-            mx_to_pairs<FMT>(w1[j], f1, b);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-              mma_bf16(sc[nt], a[0], b[0], a[1], b[1], qf[nt][4 * j], qf[nt][4 * j + 1]);
-              mma_bf16(sc[nt], a[2], b[2], a[3], b[3], qf[nt][4 * j + 2], qf[nt][4 * j + 3]);
-            }
-          }
-        }
-      }
-      // ---- softmax: a lane has keys g and g + 8 of rows 2 c and 2 c + 1
-      const int u0 = gr * kDecGranule;
-      if (u0 + kDecGranule > all_see) {
+      for (int h = 0; h < 2; ++h) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (u0 + g + 8 * (e >> 1) >= sees[nt][e & 1]) sc[nt][e] = -INFINITY;
+          for (int e = 0; e < 4; ++e) sc[h][nt][e] = 0.f;
+        uint32_t w[2][KW], f[2][B::kKPieces];
+        float key[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int p = 0; p < B::kKPieces; ++p)
+            lds_words<B::kKBytes / 4>(at + (uint32_t)(((2 * h + i) * B::kKPieces + p) * 32 + lane) * B::kKBytes, w[i] + p * (B::kKBytes / 4));
+          const uint32_t sw = scale_word(0, g + 16 * h + 8 * i);
+          uint32_t top = __vmaxu4(sw, sw >> 16);       // the largest of the row's scale bytes (head_dim 64: of two)
+          top = max(top & 0xFFu, top >> 8 & 0xFFu);
+          key[i] = mx_scale(top);                      // (NaN where a block is not finite)
+          // the lane's block(s): 32 columns from c * D / 4 on, two of 16 columns at 8 bits and head_dim 128
+          const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
+#pragma unroll
+          for (int p = 0; p < B::kKPieces; ++p) {
+            const float x = pow2_at_most_15((int)(sw >> (8 * (blk + 2 * p)) & 0xFFu) - (int)top);
+            f[i][p] = f16x2(x, x);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          constexpr int N = FMT == QUOKA_KV_MXFP8 ? 2 : 4;
+          uint32_t a[N], b[N];
+          f16_pairs<FMT>(w[0][j], f[0][j / (KW / B::kKPieces)], a);
+          f16_pairs<FMT>(w[1][j], f[1][j / (KW / B::kKPieces)], b);
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i)
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+              mma_f16(sc[h][nt], a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], qf[nt][N * j + 2 * i], qf[nt][N * j + 2 * i + 1]);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) sc[h][nt][e] *= key[e >> 1] * qs[nt][e & 1];
       }
+      // ---- softmax: a lane has keys g, g + 8, g + 16, g + 24 of rows 2 c and 2 c + 1; logits in log2 units
+      const int u0 = gr * kDecGranule;
+      if (u0 + kDecGranule > all_see) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              if (u0 + 16 * h + g + 8 * (e >> 1) >= sees[nt][e & 1]) sc[h][nt][e] = -INFINITY;
+      }
+      float top[NT][2];
       bool grow = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) grow |= fmaxf(sc[nt][e], sc[nt][e + 2]) * scale_log2 > m[nt][e] + kRescaleThreshold;
-      if (__any_sync(0xFFFFFFFFu, grow)) {              // (the reference point of the exponentials moves by more than 2^32, or is set)
+        for (int e = 0; e < 2; ++e) {
+          top[nt][e] = fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2]));
+          grow |= top[nt][e] > m[nt][e] + (float)kDecMaxAbove;
+        }
+      if (__any_sync(0xFFFFFFFFu, grow)) {              // the reference point of the exponentials is set, or moves
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            float mx = fmaxf(m[nt][e], fmaxf(sc[nt][e], sc[nt][e + 2]) * scale_log2);
+            float mx = top[nt][e];
 #pragma unroll
             for (int sh = 4; sh < 32; sh <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, sh));
+            mx = fmaxf(m[nt][e], mx - (float)kDecHeadroom);
             const float alpha = m[nt][e] == mx ? 1.f : ex2(m[nt][e] - mx);
             m[nt][e] = mx;
             l[nt][e] *= alpha;
@@ -381,50 +448,77 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
             for (int t = 0; t < TILES; ++t) { o[nt][t][e] *= alpha; o[nt][t][e + 2] *= alpha; }
           }
       }
-      uint32_t pf[NT][2];
+      uint32_t pf[2][NT][2];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const float p0 = ex2(fmaf(sc[nt][2 * h], scale_log2, -m0)), p1 = ex2(fmaf(sc[nt][2 * h + 1], scale_log2, -m1));
-          const __nv_bfloat162 p2 = __floats2bfloat162_rn(p0, p1);
-          lx[nt][0] += p0;
-          lx[nt][1] += p1;
-          const uint32_t w = *reinterpret_cast<const uint32_t*>(&p2);
-          l[nt][0] += __uint_as_float(w << 16);
-          l[nt][1] += __uint_as_float(w & 0xFFFF0000u);
-          pf[nt][h] = transpose8x8(w);
-        }
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float p0 = ex2(sc[h][nt][2 * i] - m0), p1 = ex2(sc[h][nt][2 * i + 1] - m1);
+            const uint32_t w = f16x2(p0, p1);
+            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&w));
+            lx[nt][0] += p0;
+            lx[nt][1] += p1;
+            l[nt][0] += back.x;
+            l[nt][1] += back.y;
+            pf[h][nt][i] = transpose8x8(w);
+          }
       }
       // ---- O^T += V^T P^T
-      {
-        uint32_t f[2];
-        const int blk = D == 128 ? g >> 1 : g >> 2;
+      int e[8], most = 0;                              // scale bytes of the lane's eight keys in its block of columns
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint32_t e0 = scale_word(16 + 2 * c + 8 * h) >> (8 * blk) & 0xFFu, e1 = scale_word(17 + 2 * c + 8 * h) >> (8 * blk) & 0xFFu;
-          if (e0 == kMxNanScale) nan_u = min(nan_u, u0 + 2 * c + 8 * h);
-          if (e1 == kMxNanScale) nan_u = min(nan_u, u0 + 2 * c + 8 * h + 1);
-          f[h] = (e0 == kMxNanScale ? 0u : mx_factor2<FMT>(e0) & 0xFFFFu) | (e1 == kMxNanScale ? 0u : mx_factor2<FMT>(e1) & 0xFFFF0000u);
+      for (int i = 0; i < 8; ++i) {
+        const int row = 2 * c + (i & 1) + 8 * (i >> 1);
+        e[i] = (int)(scale_word(128, row) >> (8 * (D == 128 ? g >> 1 : g >> 2)) & 0xFFu);
+        if (e[i] == (int)kMxNanScale) { nan_u = min(nan_u, u0 + row); e[i] = -200; }        // (becomes zeros)
+        most = max(most, e[i]);
+      }
+      if (__any_sync(0xFFFFFFFFu, most > ov + kDecScaleAbove || ov == 0)) {                // O's scale is set, or moves
+        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
+        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
+        if (most > ov + kDecScaleAbove || ov == 0) {
+          const float down = ov == 0 ? 0.f : pow2_at_most_15(ov - most);
+          ov = max(most, 1);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[nt][t][i] *= down;
         }
-        uint32_t v[4][VW];
+      }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kK + (uint32_t)(i * 32 + lane) * B::kVBytes, v[i]);
+      for (int h = 0; h < 2; ++h) {
+        uint32_t f[2], v[4][VW];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) f[i] = f16x2(pow2_at_most_15(e[4 * h + 2 * i] - ov), pow2_at_most_15(e[4 * h + 2 * i + 1] - ov));
+#pragma unroll
+        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kK + (uint32_t)((4 * h + i) * 32 + lane) * B::kVBytes, v[i]);
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
-          // columns of the word, the two rows of a pair side by side: 2 (4 bits: 4) and as many
+          // the word's columns, the rows of a pair side by side: x those of keys 2 c and 2 c + 1, y 8 on
+          if constexpr (FMT == QUOKA_KV_MXFP8) {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            constexpr int N = FMT == QUOKA_KV_MXFP8 ? 2 : 4;
-            uint32_t x[N], y[N];
-            mx_to_pairs<FMT>(__byte_perm(v[0][w], v[1][w], h ? 0x7632 : 0x5410), f[0], x);
-            mx_to_pairs<FMT>(__byte_perm(v[2][w], v[3][w], h ? 0x7632 : 0x5410), f[1], y);
+            for (int half = 0; half < 2; ++half) {
+              uint32_t x[2], y[2];
+              f16_pairs<FMT>(__byte_perm(v[0][w], v[1][w], half ? 0x7362 : 0x5140), f[0], x);
+              f16_pairs<FMT>(__byte_perm(v[2][w], v[3][w], half ? 0x7362 : 0x5140), f[1], y);
 #pragma unroll
-            for (int i = 0; i < N / 2; ++i)
+              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * w + half], x[0], x[1], y[0], y[1], pf[h][nt][0], pf[h][nt][1]);
+            }
+          } else {
+            constexpr uint32_t kLow = 0x0F0F0F0Fu;
+            uint32_t x0[4], x1[4], y0[4], y1[4];        // even columns, odd columns
+            f16_pairs<FMT>((v[0][w] & kLow) | (v[1][w] << 4 & ~kLow), f[0], x0);
+            f16_pairs<FMT>((v[0][w] >> 4 & kLow) | (v[1][w] & ~kLow), f[0], x1);
+            f16_pairs<FMT>((v[2][w] & kLow) | (v[3][w] << 4 & ~kLow), f[1], y0);
+            f16_pairs<FMT>((v[2][w] >> 4 & kLow) | (v[3][w] & ~kLow), f[1], y1);
 #pragma unroll
-              for (int nt = 0; nt < NT; ++nt)
-                mma_bf16(o[nt][(w * 2 + h) * (N / 2) + i], x[2 * i], x[2 * i + 1], y[2 * i], y[2 * i + 1], pf[nt][0], pf[nt][1]);
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], x0[i], x1[i], y0[i], y1[i], pf[h][nt][0], pf[h][nt][1]);
           }
         }
       }
@@ -435,6 +529,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
     // ---- the warps' results of this part
     nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 1));
     nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 2));
+    const float ov_scale = mx_scale((uint32_t)ov);
     __syncthreads();                                   // (the buffer's last part has been read)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -453,7 +548,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
           const float bad_value = __uint_as_float(0x7FC00000u);
-          to[t] = bad ? make_float2(bad_value, bad_value) : make_float2(o[nt][t][e], o[nt][t][e + 2]);
+          to[t] = bad ? make_float2(bad_value, bad_value) : make_float2(o[nt][t][e] * ov_scale, o[nt][t][e + 2] * ov_scale);
         }
       }
     __syncthreads();
@@ -476,7 +571,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       }
       if (is_whole) {
         const int r = first_row + row, h = part.kv * P.group + r % P.group, pos_r = r / P.group;
-        const float inv = kMxUnshift / sum;
+        const float inv = 1.f / sum;
         const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), b = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
         *reinterpret_cast<uint2*>(out + (long long)part.s * P.o_sb + (long long)h * P.o_sh + (long long)pos_r * P.o_st + col) =
             make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
@@ -553,7 +648,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) decode_mx_join_kernel(DevPara
       totalx = fmaf(wt, sm[w][2], totalx);
       o = fmaf(wt, so[w][col], o);
     }
-    out[(long long)s * P.o_sb + (long long)h * P.o_sh + (long long)pos * P.o_st + col] = __float2bfloat16_rn(o * (kMxUnshift / total));
+    out[(long long)s * P.o_sb + (long long)h * P.o_sh + (long long)pos * P.o_st + col] = __float2bfloat16_rn(o / total);
     if (lse && col == 0) lse[((long long)s * P.n_q + h) * P.chunk + pos] = (top + log2f(totalx)) * 0.6931471805599453f;
   }
 }
@@ -573,7 +668,7 @@ size_t decode_mx_scratch_bytes(const quoka_params* p) {
 template <int FMT, int D, int NT>
 static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt, void* out,
                                       float* lse, float* parts, cudaStream_t st, bool chained) {
-  constexpr int WARPS = kDecWarps<NT>, ROWS = 8 * NT;
+  constexpr int WARPS = kDecWarps, ROWS = 8 * NT;
   DecWork work;
   work.groups = (P.chunk * P.group + ROWS - 1) / ROWS;
   work.k_cnt = k_idx ? k_cnt : nullptr;
@@ -581,9 +676,9 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   if (sms <= 0) return cudaErrorInvalidDevice;
   const long long units = (long long)P.batch * P.n_kv * work.groups;
   const long long most = ((k_idx ? (long long)P.budget_cap : (long long)P.max_ctx) + P.chunk + kDecGranule - 1) / kDecGranule;      // granules of a unit
-  // A CTA per unit where that is three rounds of its warps or fewer, or where units are many: what joining parts costs (a launch, a
+  // A CTA per unit where that is two rounds of its warps or fewer, or where units are many: what joining parts costs (a launch, a
   // round trip through L2) is more than what the shorter rounds gain.
-  const bool whole = most <= 3 * WARPS || units >= 64ll * sms;
+  const bool whole = most <= 2 * WARPS || units >= 64ll * sms;
   const long long ctas = whole ? units : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
   if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
   const size_t smem = (size_t)WARPS * kDecStages * DecBytes<FMT, D>::kStage + (size_t)WARPS * ROWS * (D + 4 + 3) * sizeof(float);
