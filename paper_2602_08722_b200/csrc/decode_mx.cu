@@ -36,7 +36,12 @@ namespace quoka {
 using namespace ptx;
 
 constexpr int kDecGranule = 32;
-constexpr int kDecWarps = 8;
+// Warps of a CTA: what registers (168 for twelve) leave room for.  Those from kDecLast on hand their results to the others before these
+// are added up, which halves the shared memory for it: twelve rings of 8-bit rows leave 29 KB.
+template <int NT>
+constexpr int kDecWarps = NT == 2 ? 8 : 12;
+template <int NT>
+constexpr int kDecLast = NT == 2 ? 8 : 6;
 constexpr int kDecStages = 2;
 
 // What a lane copies of a granule: kKPieces pieces of kKBytes of each of four key rows, kVBytes of each of eight value rows.
@@ -94,6 +99,8 @@ __device__ __forceinline__ void f16_pairs(uint32_t w, uint32_t factor2, uint32_t
 }
 // 2^diff, diff <= 15, as an fp16 number (zero below its range).
 __device__ __forceinline__ float pow2_at_most_15(int diff) { return __uint_as_float((uint32_t)(max(diff, -60) + 127) << 23); }
+// Weight of a result with the reference point m among results whose largest is mx: what has seen nothing weighs nothing.
+__device__ __forceinline__ float dec_weight(float m, float mx) { return m == mx ? 1.f : m == -INFINITY ? 0.f : ex2(m - mx); }
 constexpr int kDecMaxAbove = 15, kDecHeadroom = 7;       // of a weight's exponent over the reference point, at most and when it is set
 constexpr int kDecScaleAbove = 7;                        // of a value block's exponent over O's: 448 * 2^7 is an fp16 number
 
@@ -202,12 +209,16 @@ struct DecPart {
   }
 };
 
+// Floats of a warp's results in the merge buffer: its rows of O, m, l and lx, or all that its lanes hold.
+template <int D, int NT>
+constexpr int dec_merge_floats() { return std::max(8 * NT * (D + 4 + 3), kDecWarps<NT> > kDecLast<NT> ? 32 * NT * (D / 4 + 6) : 0); }
+
 template <int FMT, int D, int NT>
-__global__ void __launch_bounds__(32 * kDecWarps, 1)
+__global__ void __launch_bounds__(32 * kDecWarps<NT>, 1)
 decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
                  const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units) {
   typedef DecBytes<FMT, D> B;
-  constexpr int WARPS = kDecWarps, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
+  constexpr int WARPS = kDecWarps<NT>, LAST = kDecLast<NT>, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
   constexpr int KW = B::kKBytes * B::kKPieces / 4, VW = B::kVBytes / 4;      // words of a lane per row
   constexpr int LD = D + 4;                                                  // floats of a row of the merge buffer
   extern __shared__ __align__(16) unsigned char dec_smem[];
@@ -215,8 +226,8 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   grid_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
   const uint32_t ring = smem_u32(dec_smem) + (uint32_t)warp * (ST * B::kStage);
-  float* merge = reinterpret_cast<float*>(dec_smem + (size_t)WARPS * ST * B::kStage);        // [WARPS][ROWS][LD], then m, l, lx [WARPS][ROWS]
-  float* merge_ml = merge + WARPS * ROWS * LD;
+  float* merge = reinterpret_cast<float*>(dec_smem + (size_t)WARPS * ST * B::kStage);        // [LAST][ROWS][LD], then m, l, lx [LAST][ROWS]
+  float* merge_ml = merge + LAST * ROWS * LD;
   // ---- this CTA's share
   const auto share = [&]() -> DecPart {
     if (whole_units) return DecPart(P, work, blockIdx.x);
@@ -530,27 +541,69 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
     nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 1));
     nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 2));
     const float ov_scale = mx_scale((uint32_t)ov);
-    __syncthreads();                                   // (the buffer's last part has been read)
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        float sum = l[nt][e], sumx = lx[nt][e];
 #pragma unroll
         for (int sh = 4; sh < 32; sh <<= 1) {
-          sum += __shfl_xor_sync(0xFFFFFFFFu, sum, sh);
-          sumx += __shfl_xor_sync(0xFFFFFFFFu, sumx, sh);
+          l[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, l[nt][e], sh);
+          lx[nt][e] += __shfl_xor_sync(0xFFFFFFFFu, lx[nt][e], sh);
         }
-        const int row = 8 * nt + 2 * c + e;
-        if (g == 0) { merge_ml[warp * ROWS + row] = m[nt][e]; merge_ml[(WARPS + warp) * ROWS + row] = sum; merge_ml[(2 * WARPS + warp) * ROWS + row] = sumx; }
         const bool bad = nan_u < sees[nt][e];
-        float2* to = reinterpret_cast<float2*>(merge + (warp * ROWS + row) * LD + g * (D / 8));
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-          const float bad_value = __uint_as_float(0x7FC00000u);
-          to[t] = bad ? make_float2(bad_value, bad_value) : make_float2(o[nt][t][e] * ov_scale, o[nt][t][e + 2] * ov_scale);
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) o[nt][t][e + 2 * i] = bad ? __uint_as_float(0x7FC00000u) : o[nt][t][e + 2 * i] * ov_scale;
+      }
+    __syncthreads();                                   // (the buffer's last part has been read)
+    if constexpr (WARPS > LAST) {                      // warp w + LAST's to warp w, lane by lane
+      constexpr int kValues = NT * (4 * TILES + 6);
+      float* hand = merge + (warp % LAST) * (kValues * 32) + lane;
+      if (warp >= LAST) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            hand[((nt * 2 + e) * 3) * 32] = m[nt][e]; hand[((nt * 2 + e) * 3 + 1) * 32] = l[nt][e]; hand[((nt * 2 + e) * 3 + 2) * 32] = lx[nt][e];
+          }
+#pragma unroll
+          for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) hand[(6 * NT + (nt * TILES + t) * 4 + e) * 32] = o[nt][t][e];
         }
       }
+      __syncthreads();
+      if (warp < LAST) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const float other = hand[((nt * 2 + e) * 3) * 32], mx = fmaxf(m[nt][e], other), w0 = dec_weight(m[nt][e], mx), w1 = dec_weight(other, mx);
+            m[nt][e] = mx;
+            l[nt][e] = fmaf(w1, hand[((nt * 2 + e) * 3 + 1) * 32], w0 * l[nt][e]);
+            lx[nt][e] = fmaf(w1, hand[((nt * 2 + e) * 3 + 2) * 32], w0 * lx[nt][e]);
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+              for (int i = 0; i < 2; ++i)
+                o[nt][t][e + 2 * i] = fmaf(w1, hand[(6 * NT + (nt * TILES + t) * 4 + e + 2 * i) * 32], w0 * o[nt][t][e + 2 * i]);
+          }
+      }
+      __syncthreads();
+    }
+    if (warp < LAST) {
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const int row = 8 * nt + 2 * c + e;
+          if (g == 0) { merge_ml[warp * ROWS + row] = m[nt][e]; merge_ml[(LAST + warp) * ROWS + row] = l[nt][e]; merge_ml[(2 * LAST + warp) * ROWS + row] = lx[nt][e]; }
+          float2* to = reinterpret_cast<float2*>(merge + (warp * ROWS + row) * LD + g * (D / 8));
+#pragma unroll
+          for (int t = 0; t < TILES; ++t) to[t] = make_float2(o[nt][t][e], o[nt][t][e + 2]);
+        }
+    }
     __syncthreads();
     const bool is_whole = part.begin == 0 && part.end == part.n;
     const int slot = blockIdx.x * 2 + (part.begin == 0 ? 1 : 0);
@@ -558,15 +611,15 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       const int row = i / (D / 4), col = i % (D / 4) * 4;
       float mx = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) mx = fmaxf(mx, merge_ml[w * ROWS + row]);
+      for (int w = 0; w < LAST; ++w) mx = fmaxf(mx, merge_ml[w * ROWS + row]);
       float sum = 0.f, sumx = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-      for (int w = 0; w < WARPS; ++w) {
-        const float mw = merge_ml[w * ROWS + row], wt = mw == -INFINITY && mx != -INFINITY ? 0.f : mw == mx ? 1.f : ex2(mw - mx);
+      for (int w = 0; w < LAST; ++w) {
+        const float wt = dec_weight(merge_ml[w * ROWS + row], mx);
         const float4 v = *reinterpret_cast<const float4*>(merge + (w * ROWS + row) * LD + col);
-        sum = fmaf(wt, merge_ml[(WARPS + w) * ROWS + row], sum);
-        sumx = fmaf(wt, merge_ml[(2 * WARPS + w) * ROWS + row], sumx);
+        sum = fmaf(wt, merge_ml[(LAST + w) * ROWS + row], sum);
+        sumx = fmaf(wt, merge_ml[(2 * LAST + w) * ROWS + row], sumx);
         acc.x = fmaf(wt, v.x, acc.x); acc.y = fmaf(wt, v.y, acc.y); acc.z = fmaf(wt, v.z, acc.z); acc.w = fmaf(wt, v.w, acc.w);
       }
       if (is_whole) {
@@ -606,8 +659,6 @@ __global__ void __launch_bounds__(32 * kJoinWarps) decode_mx_join_kernel(DevPara
   const int first = dec_div(a, each), last = dec_div(a + n - 1, each);
   if (first == last) return;                           // (written by that CTA)
   const auto slot = [&](int i) { return parts + (size_t)(2 * i + (i == first ? 1 : 0)) * ROWS * (D + 3); };
-  // weights of a reference point against another; what has seen nothing weighs nothing
-  const auto weight = [](float m, float mx) { return m == mx ? 1.f : m == -INFINITY ? 0.f : ex2(m - mx); };
   float mx = -INFINITY, sum = 0.f, sumx = 0.f, acc[PER];
 #pragma unroll
   for (int e = 0; e < PER; ++e) acc[e] = 0.f;
@@ -624,7 +675,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) decode_mx_join_kernel(DevPara
 #pragma unroll
     for (int j = 0; j < kJoinAtOnce; ++j)
       if (i0 + j * kJoinWarps <= last) {
-        const float top = fmaxf(mx, m[j]), w0 = weight(mx, top), w1 = weight(m[j], top);
+        const float top = fmaxf(mx, m[j]), w0 = dec_weight(mx, top), w1 = dec_weight(m[j], top);
         mx = top;
         sum = fmaf(w1, l[j], sum * w0);
         sumx = fmaf(w1, lx[j], sumx * w0);
@@ -643,7 +694,7 @@ __global__ void __launch_bounds__(32 * kJoinWarps) decode_mx_join_kernel(DevPara
     for (int w = 1; w < kJoinWarps; ++w) top = fmaxf(top, sm[w][0]);
 #pragma unroll
     for (int w = 0; w < kJoinWarps; ++w) {
-      const float wt = weight(sm[w][0], top);
+      const float wt = dec_weight(sm[w][0], top);
       total = fmaf(wt, sm[w][1], total);
       totalx = fmaf(wt, sm[w][2], totalx);
       o = fmaf(wt, so[w][col], o);
@@ -668,7 +719,7 @@ size_t decode_mx_scratch_bytes(const quoka_params* p) {
 template <int FMT, int D, int NT>
 static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const void* k, const void* v, const int32_t* k_idx, const int32_t* k_cnt, void* out,
                                       float* lse, float* parts, cudaStream_t st, bool chained) {
-  constexpr int WARPS = kDecWarps, ROWS = 8 * NT;
+  constexpr int WARPS = kDecWarps<NT>, ROWS = 8 * NT;
   DecWork work;
   work.groups = (P.chunk * P.group + ROWS - 1) / ROWS;
   work.k_cnt = k_idx ? k_cnt : nullptr;
@@ -681,7 +732,7 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   const bool whole = most <= 2 * WARPS || units >= 64ll * sms;
   const long long ctas = whole ? units : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
   if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-  const size_t smem = (size_t)WARPS * kDecStages * DecBytes<FMT, D>::kStage + (size_t)WARPS * ROWS * (D + 4 + 3) * sizeof(float);
+  const size_t smem = (size_t)WARPS * kDecStages * DecBytes<FMT, D>::kStage + (size_t)kDecLast<NT> * dec_merge_floats<D, NT>() * sizeof(float);
   cudaError_t e = cudaFuncSetAttribute(decode_mx_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   e = launch_kernel("decode_mx", decode_mx_kernel<FMT, D, NT>, dim3((unsigned)ctas), dim3(32 * WARPS), smem, st, 1, chained, P, work, (const __nv_bfloat16*)q,
