@@ -44,15 +44,20 @@ template <int NT>
 constexpr int kDecLast = NT == 2 ? 8 : 6;
 constexpr int kDecStages = 2;
 
-// What a lane copies of a granule: kKPieces pieces of kKBytes of each of four key rows, kVBytes of each of eight value rows.
+// A stage of a warp: 32 rows of K, 32 of V, 16-byte chunks swizzled as the copy engine does for rows of 128, 64 or 32 bytes (a lane's
+// reads below then meet no bank twice, or K's of 128-byte rows twice).  A lane reads kKPieces pieces of kKBytes of each of four key rows,
+// kVBytes of each of eight value rows.
 template <int FMT, int D>
 struct DecBytes {
   static constexpr int kRow = D * kMxBits<FMT> / 8;
   static constexpr int kKPieces = kRow == 128 ? 2 : 1, kKBytes = kRow / 4 / kKPieces, kVBytes = kRow / 8;
-  static constexpr uint32_t kK = 4 * kKPieces * 32 * kKBytes, kV = 8 * 32 * kVBytes;
-  static constexpr uint32_t kMeta = D == 128 ? 256 : 384;      // scale words of the rows' keys, of their values, head_dim 64 also their shifts
-  static constexpr uint32_t kStage = kK + kV + kMeta;
-  static_assert(kK == kDecGranule * kRow && kV == kDecGranule * kRow, "a granule");
+  static constexpr uint32_t kTile = kDecGranule * kRow;
+  static constexpr uint32_t kMeta = D == 128 ? 256 : 384;      // of a stage: scale words of the rows' keys, of their values, head_dim 64 also their shifts
+  static constexpr uint32_t kStage = 2 * kTile + kMeta;
+  // byte `at` of row `row` of a tile
+  static __device__ __forceinline__ uint32_t place(int row, int at) {
+    return (uint32_t)(row * kRow + (at ^ (kRow == 128 ? (row & 7) << 4 : kRow == 64 ? (row >> 1 & 3) << 4 : (row >> 2 & 1) << 4)));
+  }
 };
 
 template <int BYTES>
@@ -209,25 +214,27 @@ struct DecPart {
   }
 };
 
-// Floats of a warp's results in the merge buffer: its rows of O, m, l and lx, or all that its lanes hold.
-template <int D, int NT>
-constexpr int dec_merge_floats() { return std::max(8 * NT * (D + 4 + 3), kDecWarps<NT> > kDecLast<NT> ? 32 * NT * (D / 4 + 6) : 0); }
-
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(32 * kDecWarps<NT>, 1)
 decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-                 const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units) {
+                 const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units,
+                 const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   typedef DecBytes<FMT, D> B;
   constexpr int WARPS = kDecWarps<NT>, LAST = kDecLast<NT>, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
   constexpr int KW = B::kKBytes * B::kKPieces / 4, VW = B::kVBytes / 4;      // words of a lane per row
   constexpr int LD = D + 4;                                                  // floats of a row of the merge buffer
-  extern __shared__ __align__(16) unsigned char dec_smem[];
+  extern __shared__ unsigned char dec_smem_raw[];
+  unsigned char* dec_smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(dec_smem_raw) + 1023) & ~(uintptr_t)1023);
   grid_dependency_wait();
   grid_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, c = lane & 3;
-  const uint32_t ring = smem_u32(dec_smem) + (uint32_t)warp * (ST * B::kStage);
-  float* merge = reinterpret_cast<float*>(dec_smem + (size_t)WARPS * ST * B::kStage);        // [LAST][ROWS][LD], then m, l, lx [LAST][ROWS]
+  const uint32_t ring = smem_u32(dec_smem) + (uint32_t)warp * (ST * 2 * B::kTile);               // [WARPS][ST][K | V], then [WARPS][ST] scale words
+  const uint32_t metas = smem_u32(dec_smem) + (uint32_t)(WARPS * ST * 2) * B::kTile + (uint32_t)warp * (ST * B::kMeta);
+  uint64_t* landed = reinterpret_cast<uint64_t*>(dec_smem + WARPS * ST * B::kStage) + warp * ST;     // [WARPS][ST]
+  float* merge = reinterpret_cast<float*>(dec_smem + WARPS * ST * (B::kStage + 8));              // [LAST][ROWS][LD], then m, l, lx [LAST][ROWS]
   float* merge_ml = merge + LAST * ROWS * LD;
+  __shared__ int abort_flag;
+  const WaitCtx wc{&abort_flag, P.status};
   // ---- this CTA's share
   const auto share = [&]() -> DecPart {
     if (whole_units) return DecPart(P, work, blockIdx.x);
@@ -239,20 +246,33 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   DecPart in = share();
   if (in.begin >= in.end) return;                     // (nothing of the list is left for this CTA)
   DecPart part = in;
+  if (threadIdx.x == 0) abort_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < ST; ++i) mbar_init(&landed[i], 1);
+    fence_mbar_init();
+  }
+  __syncthreads();
   // ---- copies: granules begin + warp, + WARPS .. of every part.  A lane looks after a row: its number two granules ahead, its place one.
+  // 32 consecutive rows come through the copy engine (16-byte cp.async alone, about 20 bytes a clock and SM, held a list of 131072 rows at
+  // 4.1 TB/s); listed ones, and the last of a sequence, whose tiles end in zeros, by cp.async.
   MxPlaces places(P);
   int pos = in.begin + warp;
   bool more = true;
   int n_next, s_next = 0, kv_next = 0;                // of the granule whose places are worked out next
-  bool live_next = false;
+  bool live_next = false, run_next = false;
+  int first_next = 0;                                 // run: the first of its consecutive rows
   uint32_t place = kNoRow, srow = 0;                  // of the granule that is copied next
-  bool live = false;
+  bool live = false, run = false;
+  int first = 0, s_fill = 0, kv_fill = 0, page = 0;
   const auto ask = [&]() {
     while (more && pos >= in.end) { more = in.next(P, work); pos = in.begin + warp; }
     live_next = more;
     s_next = in.s; kv_next = in.kv;
     n_next = -1;
+    run_next = false;
     if (more) {
+      first_next = pos * kDecGranule;
+      run_next = !k_idx && first_next + kDecGranule <= in.lens.cnt + P.chunk;
       const int u = pos * kDecGranule + lane;
       if (u < in.lens.cnt) n_next = k_idx ? __ldcg(k_idx + ((long long)in.s * P.n_kv + in.kv) * P.budget_cap + u) : u;
       else if (u < in.lens.cnt + P.chunk) n_next = in.lens.T + (u - in.lens.cnt);
@@ -263,16 +283,17 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   const auto locate = [&]() {
     live = live_next;
     if (!live) return;
+    run = run_next; first = first_next; s_fill = s_next; kv_fill = kv_next;
     int t = n_next;
 #ifdef QUOKA_DEBUG
     if (t < -1 || t >= __ldg(P.ctx_len + s_next) + P.chunk) { atomicExch(P.status, (int32_t)QUOKA_ERR_BAD_INDEX); t = -1; }
 #endif
     if (s_next != s_at || kv_next != kv_at) { places.at_head(P, s_next, kv_next); s_at = s_next; kv_at = kv_next; }
-    places.of(P, t, place, srow);
+    places.of(P, t, place, srow, page);
   };
   const auto fill = [&](int stage) {
     if (live) {
-      const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV + 4 * lane;
+      const uint32_t at = ring + (uint32_t)stage * (2 * B::kTile), meta = metas + (uint32_t)stage * B::kMeta + 4 * lane;
       if (place != kNoRow) {
         const size_t word = D == 128 ? (size_t)srow * 4 : (size_t)(srow >> 1) * 4;
         cp_async_4(meta, P.k_scale + word);
@@ -281,19 +302,29 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         asm volatile("st.shared.u32 [%0], %2;\n\tst.shared.u32 [%1], %2;" ::"r"(meta), "r"(meta + 128), "r"(0u) : "memory");
       }
       if (D == 64) asm volatile("st.shared.u32 [%0], %1;" ::"r"(meta + 256), "r"((srow & 1u) * 16) : "memory");
-      constexpr int kUnit = 2 * kMxBits<FMT>;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, g + 8 * i);
-        const uint8_t* src = kc + (size_t)(row == kNoRow ? 0u : row) * kUnit + c * B::kKBytes;
-#pragma unroll
-        for (int p = 0; p < B::kKPieces; ++p)          // (pieces 64 bytes apart: a warp asks for every sector once)
-          cp_async_n<B::kKBytes>(at + (uint32_t)((i * B::kKPieces + p) * 32 + lane) * B::kKBytes, src + 64 * p, row != kNoRow);
-      }
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {                    // keys 2 c, 2 c + 1, and 8 on, of both halves of the granule
-        const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, 2 * c + (i & 1) + 8 * (i >> 1));
-        cp_async_n<B::kVBytes>(at + B::kK + (uint32_t)(i * 32 + lane) * B::kVBytes, vc + (size_t)(row == kNoRow ? 0u : row) * kUnit + g * B::kVBytes, row != kNoRow);
+      if (run) {
+        if (lane == 0) {
+          fence_proxy_async_smem();                   // earlier contents of the stage were read, or written, through the generic proxy
+          mbar_arrive_expect_tx(&landed[stage], 2 * B::kTile);
+          int c1 = first, c3 = s_fill;
+          if (P.page_size != 0) { c3 = page; c1 = first & (kPage - 1); }
+          unsigned char* dst = dec_smem + ((size_t)warp * ST + stage) * (2 * B::kTile);
+          tma_load_4d(dst, &tm_k, &landed[stage], 0, c1, kv_fill, c3);
+          tma_load_4d(dst + B::kTile, &tm_v, &landed[stage], 0, c1, kv_fill, c3);
+        }
+      } else {
+        constexpr int kUnit = 2 * kMxBits<FMT>;
+#pragma unroll 1                                     // (few instructions: this is not the long lists' path, or it waits for memory)
+        for (int i = 0; i < 8; ++i) {
+          const int rv = 2 * c + (i & 1) + 8 * (i >> 1);           // keys 2 c, 2 c + 1, and 8 on, of both halves of the granule
+          const uint32_t row = __shfl_sync(0xFFFFFFFFu, place, rv);
+          cp_async_n<B::kVBytes>(at + B::kTile + B::place(rv, g * B::kVBytes), vc + (size_t)(row == kNoRow ? 0u : row) * kUnit + g * B::kVBytes, row != kNoRow);
+          const int rk = g + 8 * (i >> 1), piece = c * B::kKBytes + 64 * (i & 1);
+          const uint32_t rowk = __shfl_sync(0xFFFFFFFFu, place, rk);
+          if (i % 2 < B::kKPieces)                     // (pieces 64 bytes apart: a warp asks for every sector once)
+            cp_async_n<B::kKBytes>(at + B::place(rk, piece), kc + (size_t)(rowk == kNoRow ? 0u : rowk) * kUnit + piece, rowk != kNoRow);
+        }
+        if (lane == 0) mbar_arrive(&landed[stage]);
       }
     }
     cp_async_commit();
@@ -310,6 +341,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   float qs[NT][2];                                    // to log2 units of the logits, of the rows of this lane's columns
   float o[NT][TILES][4], m[NT][2], l[NT][2], lx[NT][2];    // lx: the sum of the weights before they are rounded
   int stage = 0, s_cur = -1, kv_cur = -1, grp_cur = -1;
+  uint32_t phase = 0;
   for (bool again = true; again;) {
     const int first_row = part.grp * ROWS, n_rows = min(ROWS, P.chunk * P.group - first_row);
     // ---- the part's query rows
@@ -365,8 +397,9 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll 1
     for (int gr = part.begin + warp; gr < part.end; gr += WARPS) {
       cp_async_wait<ST - 1>();
+      if (!mbar_wait_done(&landed[stage], phase, wc)) break;
       __syncwarp();
-      const uint32_t at = ring + (uint32_t)stage * B::kStage, meta = at + B::kK + B::kV;
+      const uint32_t at = ring + (uint32_t)stage * (2 * B::kTile), meta = metas + (uint32_t)stage * B::kMeta;
       // scale bytes of the i-th row's keys (0) or values (128)
       const auto scale_word = [&](int what, int i) {
         uint32_t w;
@@ -392,7 +425,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         for (int i = 0; i < 2; ++i) {
 #pragma unroll
           for (int p = 0; p < B::kKPieces; ++p)
-            lds_words<B::kKBytes / 4>(at + (uint32_t)(((2 * h + i) * B::kKPieces + p) * 32 + lane) * B::kKBytes, w[i] + p * (B::kKBytes / 4));
+            lds_words<B::kKBytes / 4>(at + B::place(g + 16 * h + 8 * i, c * B::kKBytes + 64 * p), w[i] + p * (B::kKBytes / 4));
           const uint32_t sw = scale_word(0, g + 16 * h + 8 * i);
           uint32_t top = __vmaxu4(sw, sw >> 16);       // the largest of the row's scale bytes (head_dim 64: of two)
           top = max(top & 0xFFu, top >> 8 & 0xFFu);
@@ -506,7 +539,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
         for (int i = 0; i < 2; ++i) f[i] = f16x2(pow2_at_most_15(e[4 * h + 2 * i] - ov), pow2_at_most_15(e[4 * h + 2 * i + 1] - ov));
 #pragma unroll
-        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kK + (uint32_t)((4 * h + i) * 32 + lane) * B::kVBytes, v[i]);
+        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kTile + B::place(16 * h + 2 * c + (i & 1) + 8 * (i >> 1), g * B::kVBytes), v[i]);
 #pragma unroll
         for (int w = 0; w < VW; ++w) {
           // the word's columns, the rows of a pair side by side: x those of keys 2 c and 2 c + 1, y 8 on
@@ -535,7 +568,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       }
       __syncwarp();                                    // the scale words of this stage have been read
       fill(stage);
-      if (++stage == ST) stage = 0;
+      if (++stage == ST) { stage = 0; phase ^= 1; }
     }
     // ---- the warps' results of this part
     nan_u = min(nan_u, __shfl_xor_sync(0xFFFFFFFFu, nan_u, 1));
@@ -558,19 +591,23 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       }
     __syncthreads();                                   // (the buffer's last part has been read)
     if constexpr (WARPS > LAST) {                      // warp w + LAST's to warp w, lane by lane
-      constexpr int kValues = NT * (4 * TILES + 6);
+      constexpr int kValues = NT * 4 * TILES;
+      static_assert(kValues * 32 <= ROWS * LD, "what a warp's rows take below");
       float* hand = merge + (warp % LAST) * (kValues * 32) + lane;
+      float* hand_ml = merge_ml + warp % LAST * ROWS + 2 * c;
       if (warp >= LAST) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
+          if (g == 0) {
 #pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            hand[((nt * 2 + e) * 3) * 32] = m[nt][e]; hand[((nt * 2 + e) * 3 + 1) * 32] = l[nt][e]; hand[((nt * 2 + e) * 3 + 2) * 32] = lx[nt][e];
+            for (int e = 0; e < 2; ++e) {
+              hand_ml[8 * nt + e] = m[nt][e]; hand_ml[LAST * ROWS + 8 * nt + e] = l[nt][e]; hand_ml[2 * LAST * ROWS + 8 * nt + e] = lx[nt][e];
+            }
           }
 #pragma unroll
           for (int t = 0; t < TILES; ++t)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) hand[(6 * NT + (nt * TILES + t) * 4 + e) * 32] = o[nt][t][e];
+            for (int e = 0; e < 4; ++e) hand[((nt * TILES + t) * 4 + e) * 32] = o[nt][t][e];
         }
       }
       __syncthreads();
@@ -579,15 +616,14 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 2; ++e) {
-            const float other = hand[((nt * 2 + e) * 3) * 32], mx = fmaxf(m[nt][e], other), w0 = dec_weight(m[nt][e], mx), w1 = dec_weight(other, mx);
+            const float other = hand_ml[8 * nt + e], mx = fmaxf(m[nt][e], other), w0 = dec_weight(m[nt][e], mx), w1 = dec_weight(other, mx);
             m[nt][e] = mx;
-            l[nt][e] = fmaf(w1, hand[((nt * 2 + e) * 3 + 1) * 32], w0 * l[nt][e]);
-            lx[nt][e] = fmaf(w1, hand[((nt * 2 + e) * 3 + 2) * 32], w0 * lx[nt][e]);
+            l[nt][e] = fmaf(w1, hand_ml[LAST * ROWS + 8 * nt + e], w0 * l[nt][e]);
+            lx[nt][e] = fmaf(w1, hand_ml[2 * LAST * ROWS + 8 * nt + e], w0 * lx[nt][e]);
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
-              for (int i = 0; i < 2; ++i)
-                o[nt][t][e + 2 * i] = fmaf(w1, hand[(6 * NT + (nt * TILES + t) * 4 + e + 2 * i) * 32], w0 * o[nt][t][e + 2 * i]);
+              for (int i = 0; i < 2; ++i) o[nt][t][e + 2 * i] = fmaf(w1, hand[((nt * TILES + t) * 4 + e + 2 * i) * 32], w0 * o[nt][t][e + 2 * i]);
           }
       }
       __syncthreads();
@@ -732,11 +768,13 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   const bool whole = most <= 2 * WARPS || units >= 64ll * sms;
   const long long ctas = whole ? units : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
   if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-  const size_t smem = (size_t)WARPS * kDecStages * DecBytes<FMT, D>::kStage + (size_t)kDecLast<NT> * dec_merge_floats<D, NT>() * sizeof(float);
+  CUtensorMap tm_k, tm_v;
+  if (!encode_mx_tile_map(&tm_k, P, FMT, k, kDecGranule) || !encode_mx_tile_map(&tm_v, P, FMT, v, kDecGranule)) return cudaErrorInvalidValue;
+  const size_t smem = 1024 + (size_t)WARPS * kDecStages * (DecBytes<FMT, D>::kStage + 8) + (size_t)kDecLast<NT> * ROWS * (D + 4 + 3) * sizeof(float);
   cudaError_t e = cudaFuncSetAttribute(decode_mx_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
   e = launch_kernel("decode_mx", decode_mx_kernel<FMT, D, NT>, dim3((unsigned)ctas), dim3(32 * WARPS), smem, st, 1, chained, P, work, (const __nv_bfloat16*)q,
-                    (const uint8_t*)k, (const uint8_t*)v, k_idx, (__nv_bfloat16*)out, lse, parts, whole ? 1 : 0);
+                    (const uint8_t*)k, (const uint8_t*)v, k_idx, (__nv_bfloat16*)out, lse, parts, whole ? 1 : 0, tm_k, tm_v);
   if (e != cudaSuccess) return e;
   count_launch();
   if (!whole) {

@@ -53,32 +53,39 @@ __device__ __forceinline__ void store_codes(uint8_t* row, int piece, const uint3
   else reinterpret_cast<uint32_t*>(row)[piece] = w[0];
 }
 
-template <typename E, int FMT, int D>
+// A CTA takes UNR * 256 / LPR rows of a (sequence, KV head), a thread the same piece of UNR of them, all loads before their first use.
+template <typename E, int FMT, int D, int UNR>
 __global__ void __launch_bounds__(kMxThreads) append_kv_mx_kernel(DevParams P, const E* __restrict__ k_new, const E* __restrict__ v_new,
                                                                   uint8_t* __restrict__ k_cache, uint8_t* __restrict__ v_cache,
                                                                   uint8_t* __restrict__ k_scale, uint8_t* __restrict__ v_scale,
-                                                                  float* __restrict__ k_inv_norm) {
+                                                                  float* __restrict__ k_inv_norm, int tiles) {
   grid_dependency_wait();
   grid_launch_dependents();
-  constexpr int LPR = D / 8;                         // lanes per row: 8 or 16
-  const int64_t total = (int64_t)P.batch * P.n_kv * P.chunk * LPR;
-  const int lane = threadIdx.x & 31, c = lane % LPR;
-  for (int64_t e0 = (int64_t)blockIdx.x * kMxThreads + threadIdx.x - lane; e0 < total; e0 += (int64_t)gridDim.x * kMxThreads) {
-    const bool live = e0 + lane < total;             // (whole rows: LPR divides a warp)
-    const int64_t row = live ? (e0 + lane) / LPR : 0;
-    const int r = (int)(row % P.chunk), h = (int)(row / P.chunk % P.n_kv), s = (int)(row / ((int64_t)P.chunk * P.n_kv));
-    float kx[8], vx[8];
-    load8(k_new + row * D + c * 8, kx);
-    load8(v_new + row * D + c * 8, vx);
-    const int t = load_input<true>(P.ctx_len + s) + r;
+  constexpr int LPR = D / 8, RPP = kMxThreads / LPR;  // lanes per row (8 or 16), rows per pass
+  const int c = threadIdx.x % LPR, unit = blockIdx.x / tiles, r0 = blockIdx.x % tiles * (UNR * RPP) + threadIdx.x / LPR;
+  const int h = unit % P.n_kv, s = unit / P.n_kv;
+  const int64_t first = (int64_t)unit * P.chunk;
+  const int T = load_input<true>(P.ctx_len + s);
+  float kx[UNR][8], vx[UNR][8];
+#pragma unroll
+  for (int j = 0; j < UNR; ++j) {                     // (a row past the chunk reads the last one; it is not written)
+    const int64_t row = first + min(r0 + j * RPP, P.chunk - 1);
+    load8(k_new + row * D + c * 8, kx[j]);
+    load8(v_new + row * D + c * 8, vx[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < UNR; ++j) {
+    const int r = r0 + j * RPP, t = T + r;
     uint32_t kw[2], vw[2];
-    const uint32_t kb = mx_quantise8<FMT>(kx, kw), vb = mx_quantise8<FMT>(vx, vw);
+    const uint32_t kb = mx_quantise8<FMT>(kx[j], kw), vb = mx_quantise8<FMT>(vx[j], vw);
     float nn = 0.f;
+    if (k_inv_norm != nullptr) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) nn = fmaf(kx[i], kx[i], nn);
+      for (int i = 0; i < 8; ++i) nn = fmaf(kx[j][i], kx[j][i], nn);
 #pragma unroll
-    for (int o = LPR / 2; o > 0; o >>= 1) nn += __shfl_xor_sync(0xFFFFFFFFu, nn, o);
-    if (!live) continue;
+      for (int o = LPR / 2; o > 0; o >>= 1) nn += __shfl_xor_sync(0xFFFFFFFFu, nn, o);
+    }
+    if (r >= P.chunk) continue;
     const int64_t off = kv_row_offset<true>(P, s, h, t) * kMxBits<FMT> / 8;
     store_codes<FMT>(k_cache + off, c, kw);
     store_codes<FMT>(v_cache + off, c, vw);
@@ -91,18 +98,18 @@ __global__ void __launch_bounds__(kMxThreads) append_kv_mx_kernel(DevParams P, c
   }
 }
 
-// 8 elements of a row (a piece) as the values they stand for.
+// 8 elements of a row (a piece), and the values they stand for.
 template <int FMT>
-__device__ __forceinline__ void load_values8(const uint8_t* row, int piece, float scale, float (&x)[8]) {
-  if constexpr (FMT == QUOKA_KV_MXFP8) {
-    const uint2 w = load_input<true>(reinterpret_cast<const uint2*>(row) + piece);
-    const uint32_t v[2] = {w.x, w.y};
+__device__ __forceinline__ uint2 load_piece(const uint8_t* row, int piece) {
+  if constexpr (FMT == QUOKA_KV_MXFP8) return load_input<true>(reinterpret_cast<const uint2*>(row) + piece);
+  else return make_uint2(load_input<true>(reinterpret_cast<const uint32_t*>(row) + piece), 0u);
+}
+template <int FMT>
+__device__ __forceinline__ void piece_values(uint2 w, float scale, float (&x)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = mx_element<FMT>(v[i / 4] >> (8 * (i % 4)) & 0xFFu) * scale;
-  } else {
-    const uint32_t v = load_input<true>(reinterpret_cast<const uint32_t*>(row) + piece);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = mx_element<FMT>(v >> (4 * i) & 0xFu) * scale;
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t code = FMT == QUOKA_KV_MXFP8 ? (i < 4 ? w.x : w.y) >> (8 * (i % 4)) & 0xFFu : w.x >> (4 * i) & 0xFu;
+    x[i] = mx_element<FMT>(code) * scale;
   }
 }
 template <typename E>
@@ -121,46 +128,66 @@ __device__ __forceinline__ void store8(E* p, const float (&x)[8]) {
   }
 }
 
-template <typename E, int FMT, int D>
+template <typename E, int FMT, int D, int UNR>
 __global__ void __launch_bounds__(kMxThreads) read_kv_mx_kernel(DevParams P, const uint8_t* __restrict__ k_cache,
                                                                 const uint8_t* __restrict__ v_cache, int first, int n_rows,
-                                                                E* __restrict__ k_out, E* __restrict__ v_out) {
+                                                                E* __restrict__ k_out, E* __restrict__ v_out, int tiles) {
   grid_dependency_wait();
   grid_launch_dependents();
-  constexpr int LPR = D / 8;
-  const int64_t total = (int64_t)P.batch * P.n_kv * n_rows * LPR;
-  for (int64_t e = (int64_t)blockIdx.x * kMxThreads + threadIdx.x; e < total; e += (int64_t)gridDim.x * kMxThreads) {
-    const int64_t row = e / LPR;
-    const int c = (int)(e % LPR);
-    const int r = (int)(row % n_rows), h = (int)(row / n_rows % P.n_kv), s = (int)(row / ((int64_t)n_rows * P.n_kv));
-    const int T = load_input<true>(P.ctx_len + s);
-    const int64_t t = (int64_t)(first < 0 ? T : first) + r;
-    if (t >= (int64_t)T + P.chunk) continue;
-    const int64_t off = kv_row_offset<true>(P, s, h, (int)t) * kMxBits<FMT> / 8;
-    const int64_t at = mx_scale_index<D, true>(P, s, h, (int)t) + c / 4;
-    float x[8], y[8];
-    load_values8<FMT>(k_cache + off, c, mx_scale(load_input<true>(P.k_scale + at)), x);
-    if (v_cache) load_values8<FMT>(v_cache + off, c, mx_scale(load_input<true>(P.v_scale + at)), y);
-    store8(k_out + row * D + c * 8, x);
-    if (v_cache) store8(v_out + row * D + c * 8, y);
+  constexpr int LPR = D / 8, RPP = kMxThreads / LPR;
+  const int c = threadIdx.x % LPR, unit = blockIdx.x / tiles, r0 = blockIdx.x % tiles * (UNR * RPP) + threadIdx.x / LPR;
+  const int h = unit % P.n_kv, s = unit / P.n_kv;
+  const int T = load_input<true>(P.ctx_len + s);
+  const int64_t t0 = first < 0 ? T : first;
+  const int64_t rows = min((int64_t)n_rows, (int64_t)T + P.chunk - t0);      // that there are
+  if (r0 >= rows) return;
+  uint2 kw[UNR], vw[UNR];
+  uint8_t kb[UNR], vb[UNR];
+#pragma unroll
+  for (int j = 0; j < UNR; ++j) {                     // (a row past them reads the last one; it is not written)
+    const int t = (int)(t0 + min((int64_t)r0 + j * RPP, rows - 1));
+    const int64_t off = kv_row_offset<true>(P, s, h, t) * kMxBits<FMT> / 8;
+    const int64_t at = mx_scale_index<D, true>(P, s, h, t) + c / 4;
+    kw[j] = load_piece<FMT>(k_cache + off, c);
+    kb[j] = load_input<true>(P.k_scale + at);
+    if (v_cache) { vw[j] = load_piece<FMT>(v_cache + off, c); vb[j] = load_input<true>(P.v_scale + at); }
+  }
+#pragma unroll
+  for (int j = 0; j < UNR; ++j) {
+    if (r0 + j * RPP >= rows) break;
+    const int64_t to = ((int64_t)unit * n_rows + r0 + j * RPP) * D + c * 8;
+    float x[8];
+    piece_values<FMT>(kw[j], mx_scale(kb[j]), x);
+    store8(k_out + to, x);
+    if (v_cache) {
+      piece_values<FMT>(vw[j], mx_scale(vb[j]), x);
+      store8(v_out + to, x);
+    }
   }
 }
 
 // ---------------------------------------------------------------------------------------------- host
-static unsigned mx_blocks(int64_t threads) {
-  int64_t blocks = (threads + kMxThreads - 1) / kMxThreads;
-  const int64_t most = 16ll * device_sm_count();                     // two waves of eight CTAs per SM; longer ones loop
-  if (blocks > most && most > 0) blocks = most;
-  return (unsigned)blocks;
+// Rows per thread: four where the CTAs then still make two waves, else one.
+struct MxGrid { int unr, tiles; int64_t ctas; };
+static MxGrid mx_grid(const DevParams& P, int64_t rows) {
+  const int64_t units = (int64_t)P.batch * P.n_kv;
+  const auto of = [&](int unr) {
+    const int per = unr * kMxThreads / (P.d / 8);
+    const int64_t tiles = (rows + per - 1) / per;
+    return MxGrid{unr, (int)tiles, tiles * units};
+  };
+  const MxGrid four = of(4);
+  return four.ctas >= 2ll * device_sm_count() ? four : of(1);
 }
 
 cudaError_t launch_append_kv_mx(const DevParams& P, int dtype, int fmt, const void* k_new, const void* v_new, void* k_cache, void* v_cache,
                                 uint8_t* k_scale, uint8_t* v_scale, float* k_inv_norm, cudaStream_t st) {
-  const dim3 grid(mx_blocks((int64_t)P.batch * P.n_kv * P.chunk * (P.d / 8)));
+  const MxGrid g = mx_grid(P, P.chunk);
+  if (g.ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
   const cudaError_t e = mx_dispatch(dtype, fmt, P.d, [&](auto elem, auto f, auto d) {
     using E = decltype(elem);
-    return launch_kernel("append_kv_mx", append_kv_mx_kernel<E, f.value, d.value>, grid, dim3(kMxThreads), 0, st, 1, true, P, (const E*)k_new,
-                         (const E*)v_new, (uint8_t*)k_cache, (uint8_t*)v_cache, k_scale, v_scale, k_inv_norm);
+    return launch_kernel("append_kv_mx", g.unr == 4 ? append_kv_mx_kernel<E, f.value, d.value, 4> : append_kv_mx_kernel<E, f.value, d.value, 1>, dim3((unsigned)g.ctas),
+                         dim3(kMxThreads), 0, st, 1, true, P, (const E*)k_new, (const E*)v_new, (uint8_t*)k_cache, (uint8_t*)v_cache, k_scale, v_scale, k_inv_norm, g.tiles);
   });
   if (e != cudaSuccess) return e;
   count_launch();
@@ -169,11 +196,12 @@ cudaError_t launch_append_kv_mx(const DevParams& P, int dtype, int fmt, const vo
 
 cudaError_t launch_read_kv_mx(const DevParams& P, int dtype, int fmt, const void* k_cache, const void* v_cache, int first, int n_rows,
                               void* k_out, void* v_out, cudaStream_t st) {
-  const dim3 grid(mx_blocks((int64_t)P.batch * P.n_kv * n_rows * (P.d / 8)));
+  const MxGrid g = mx_grid(P, n_rows);
+  if (g.ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
   const cudaError_t e = mx_dispatch(dtype, fmt, P.d, [&](auto elem, auto f, auto d) {
     using E = decltype(elem);
-    return launch_kernel("read_kv_mx", read_kv_mx_kernel<E, f.value, d.value>, grid, dim3(kMxThreads), 0, st, 1, true, P, (const uint8_t*)k_cache,
-                         (const uint8_t*)v_cache, first, n_rows, (E*)k_out, (E*)v_out);
+    return launch_kernel("read_kv_mx", g.unr == 4 ? read_kv_mx_kernel<E, f.value, d.value, 4> : read_kv_mx_kernel<E, f.value, d.value, 1>, dim3((unsigned)g.ctas),
+                         dim3(kMxThreads), 0, st, 1, true, P, (const uint8_t*)k_cache, (const uint8_t*)v_cache, first, n_rows, (E*)k_out, (E*)v_out, g.tiles);
   });
   if (e != cudaSuccess) return e;
   count_launch();

@@ -200,12 +200,14 @@ struct MxPlaces {
     table = P.block_table + (long long)s * P.max_pages;
   }
   // t < 0: kNoRow
-  __device__ __forceinline__ void of(const DevParams& P, int t, uint32_t& place, uint32_t& srow) const {
+  __device__ __forceinline__ void of(const DevParams& P, int t, uint32_t& place, uint32_t& srow) const { int page; of(P, t, place, srow, page); }
+  __device__ __forceinline__ void of(const DevParams& P, int t, uint32_t& place, uint32_t& srow, int& page) const {
+    page = 0;
     const int tc = max(t, 0);
     uint32_t off = (uint32_t)tc * st;
     srow = srow0 + (uint32_t)tc;
     if (P.page_size != 0) {
-      int page = __ldg(table + (tc >> 6));
+      page = __ldg(table + (tc >> 6));
 #ifdef QUOKA_DEBUG
       // debug build: a page id outside the pool is recorded and the row treated as absent
       if (page < 0 || (long long)page >= P.kv_rows) {

@@ -504,6 +504,18 @@ bool encode_mx_tensor_map(CUtensorMap* out, const quoka_params* p, int fmt, cons
             CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+bool encode_mx_tile_map(CUtensorMap* out, const DevParams& P, int fmt, const void* cache, int rows) {
+  EncodeTiledFn fn = get_encode_fn();
+  if (!fn) return false;
+  const int bits = fmt == QUOKA_KV_MXFP8 ? 8 : 4, row = P.d * bits / 8;
+  const cuuint64_t dims[4] = {(cuuint64_t)row, (cuuint64_t)(P.page_size ? kPage : P.kv_rows), (cuuint64_t)P.n_kv, (cuuint64_t)(P.page_size ? P.kv_rows : P.batch)};
+  const cuuint64_t strides[3] = {(cuuint64_t)P.kv_st * bits / 8, (cuuint64_t)P.kv_sh * bits / 8, (cuuint64_t)P.kv_sb * bits / 8};
+  const cuuint32_t box[4] = {(cuuint32_t)row, (cuuint32_t)rows, 1, 1}, one[4] = {1, 1, 1, 1};
+  return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(cache), dims, strides, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            row == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : row == 64 ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_32B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+            CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
 bool score_keys_tc_supported(const quoka_params* p) {
   if (p->dtype != QUOKA_BF16) return false;
   const int N = p->n_retain < p->chunk_len ? p->n_retain : p->chunk_len;

@@ -44,6 +44,8 @@ quoka_status launch_attn_tc_pair(const quoka_params* p, const DevParams& P, cons
 // The same over a microscaled cache (the scale arrays in P).
 // raw rows of the cache, `cols` columns, in boxes of 64 rows
 bool encode_mx_tensor_map(CUtensorMap* out, const quoka_params* p, int fmt, const void* cache, int cols);
+// whole raw rows in boxes of `rows`, chunks swizzled over the row's 128, 64 or 32 bytes
+bool encode_mx_tile_map(CUtensorMap* out, const DevParams& P, int fmt, const void* cache, int rows);
 bool score_keys_mx_tc_supported(const quoka_params* p);
 quoka_status launch_score_keys_mx_tc(const quoka_params* p, const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st,
                                      bool chained);
