@@ -29,6 +29,10 @@ static DevParams make_dev_mx(const quoka_params* p, const quoka_mx_cache* mx, vo
 static quoka_status run_score_keys_mx(const quoka_params* p, const quoka_mx_cache* mx, const DevParams& P, const void* qbar, const void* k,
                                       float* scores, cudaStream_t st, bool chained = false) {
   if (p->max_ctx_len == 0) return QUOKA_OK;
+  if (p->impl == QUOKA_IMPL_AUTO && score_keys_mx_tc_supported(p) && score_few_mx_applies(p)) {
+    QUOKA_TRY_CUDA(launch_score_few_mx(P, mx->format, qbar, k, scores, st, chained));
+    return QUOKA_OK;
+  }
   if (p->impl != QUOKA_IMPL_SIMT && score_keys_mx_tc_supported(p)) return launch_score_keys_mx_tc(p, P, mx->format, qbar, k, scores, st, chained);
   if (p->impl == QUOKA_IMPL_TENSOR) return QUOKA_ERR_UNSUPPORTED;
   QUOKA_TRY_CUDA(launch_score_keys_mx_simt(P, p->dtype, mx->format, qbar, k, scores, st));

@@ -29,6 +29,9 @@ cudaError_t launch_score_keys_mx_simt(const DevParams& P, int dtype, int fmt, co
 cudaError_t launch_attn_mx_simt(const DevParams& P, int dtype, int fmt, const void* q, const void* k, const void* v, const int32_t* k_idx,
                                 const int32_t* k_cnt, void* out, float* lse, cudaStream_t st);
 
+// Eight retained queries or fewer (score_few_mx.cu)
+bool score_few_mx_applies(const quoka_params* p);
+cudaError_t launch_score_few_mx(const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st, bool chained);
 // A few query rows per KV head (decode_mx.cu); parts: scratch of decode_mx_scratch_bytes
 bool decode_mx_applies(const quoka_params* p);
 size_t decode_mx_scratch_bytes(const quoka_params* p);
