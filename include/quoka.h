@@ -275,8 +275,8 @@ typedef enum { QUOKA_KV_MXFP8 = 1, QUOKA_KV_MXFP4 = 2 } quoka_kv_format;
 typedef struct {
   int32_t format;      /* quoka_kv_format */
   uint8_t* k_scale;    /* DEVICE scale bytes of the keys and values, head_dim / 32 per row, indexed like the cache without head_dim:  */
-  uint8_t* v_scale;    /* contiguous [b][n_KV][kv_rows][head_dim / 32], paged [page][n_KV][64][head_dim / 32]; 16-byte aligned.
-                          Only quoka_append_kv_mx writes them. */
+  uint8_t* v_scale;    /* contiguous [b][n_KV][kv_rows][head_dim / 32], paged [page][n_KV][64][head_dim / 32]; 16-byte aligned, and
+                          allocated to a multiple of 4 bytes (whole words are read).  Only quoka_append_kv_mx writes them. */
 } quoka_mx_cache;
 
 /* Workspace of the calls below, in the manner of quoka_workspace_size. */

@@ -158,12 +158,15 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
   const DevParams P = make_dev_mx(p, mx, ws, w);
   int32_t* k_idx = k_idx_out ? k_idx_out : w.k_idx;
   int32_t* k_cnt = k_cnt_out ? k_cnt_out : w.k_cnt;
+  // The chain of launches of the bf16 call.
   if (p->max_ctx_len > 0) {
-    if ((st = run_select_queries(p, P, q, w.q_idx, w.qbar, cs)) != QUOKA_OK) return st;
-    if ((st = run_score_keys_mx(p, mx, P, w.qbar, k_cache, w.scores, cs)) != QUOKA_OK) return st;
+    if ((st = run_select_queries(p, P, q, w.q_idx, w.qbar, cs, attn_below_a_wave(p))) != QUOKA_OK) return st;
+    if ((st = run_score_keys_mx(p, mx, P, w.qbar, k_cache, w.scores, cs, /*chained=*/true)) != QUOKA_OK) return st;
+  } else if (P.attn_counters) {
+    QUOKA_TRY_CUDA(cudaMemsetAsync(P.attn_counters, 0, P.n_attn_counters * sizeof(int32_t), cs));
   }
-  QUOKA_TRY_CUDA(launch_select_keys(P, w.scores, k_idx, k_cnt, cs));
-  return run_attn_mx(p, mx, P, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs, plan);
+  QUOKA_TRY_CUDA(launch_select_keys(P, w.scores, k_idx, k_cnt, cs, /*chained=*/p->max_ctx_len > 0));
+  return run_attn_mx(p, mx, P, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs, plan, /*after_selection=*/true);
 }
 
 }  // extern "C"

@@ -258,6 +258,134 @@ def test_blocks_that_are_not_finite_reach_only_the_rows_that_see_them(impl, use_
     assert (np.abs(got - out)[rows_clean] <= bound[rows_clean]).all()
 
 
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n_q,n_kv,d,T,C,bad_k,bad_v", [
+    # row blocks whose key tiles are cut into parts (in a cluster, through memory), and shares of several CTAs
+    (8, 2, 128, 3000, 64, [], [(2999, 0), (3040, 2)]), (8, 2, 128, 3000, 64, [(3010, 1)], [(17, 3)]), (4, 1, 64, 4000, 100, [], [(4050, 1), (4090, 0)]),
+    (8, 2, 128, 2500, 1, [], [(2500, 3)]), (8, 2, 64, 2500, 2, [(2501, 1)], [(2501, 0)]), (16, 4, 128, 2100, 7, [(2103, 0)], [(2105, 1), (40, 2)])])
+def test_blocks_that_are_not_finite_in_calls_cut_into_parts(use_list, fmt, n_q, n_kv, d, T, C, bad_k, bad_v):
+    test_blocks_that_are_not_finite_reach_only_the_rows_that_see_them(api.IMPL_AUTO, use_list, fmt, 1, n_q, n_kv, d, T, C, bad_k, bad_v)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("N,norms,agg", [(1, False, "max"), (5, True, "max"), (8, False, "mean"), (40, False, "max"), (40, True, "mean")])
+def test_keys_that_are_not_finite_score_minus_infinity(fmt, N, norms, agg):
+    inp = synth.make_chunk_inputs(6, 1, 4, 2, 128, [300], N, "bf16")
+    inp.k[0, 0, 7, 3] = float("nan")
+    inp.k[0, 1, 299, 100] = float("-inf")
+    g = torch.Generator().manual_seed(8)
+    qbar = torch.randn(1, 2, N, 128, generator=g)
+    qbar = (qbar / qbar.norm(dim=-1, keepdim=True)).bfloat16().cuda()
+    for impl in IMPLS:
+        P = R.MxProblem(inp, fmt, n_retain=N, kv_budget=8, impl=impl)
+        if norms:
+            P.norms = torch.zeros(P.k.shape[:3], device="cuda")
+            n = torch.from_numpy(1.0 / np.fmax(np.sqrt((P.k64 ** 2).sum(-1)), 1e-12)).float()
+            P.norms.copy_(n)
+            P.p.k_inv_norm = P.norms.data_ptr()
+        P.p.query_agg = {"max": api.AGG_MAX, "mean": api.AGG_MEAN}[agg]
+        scores = torch.full((1, 2, P.max_ctx), 7.0, device="cuda")
+        api.quoka_score_keys_mx(P.p, P.mx, qbar, P.k, scores, P.ws)
+        got = scores.double().cpu().numpy()
+        for h, t in ((0, 7), (1, 299)):
+            assert np.isnan(got[0, h, t]) if agg == "mean" else got[0, h, t] == -np.inf
+            got[0, h, t] = 0
+        want = O.score_keys(qbar[0].double().cpu().numpy(), np.nan_to_num(P.k64[0, :, :300]), 300, "cosine", agg)
+        want[0, 7] = want[1, 299] = 0
+        assert np.abs(got[0] - want).max() <= PA.SCORE_ATOL
+
+
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("n_q,n_kv,d,lens,C,paged", [
+    (8, 2, 128, [900, 130], 300, True), (32, 8, 128, [2000], 256, False), (8, 2, 64, [700], 200, True), (8, 8, 128, [5000], 40, False)])
+def test_long_chunks_are_the_bf16_call_on_what_the_cache_reads_as(use_list, n_q, n_kv, d, lens, C, paged):
+    """Every value of the cache is a bf16 number: the tensor-core kernels of chunks give what they give over a bf16 cache of them,
+    up to the order in which 16 columns of a product are added up."""
+    b = len(lens)
+    inp = synth.make_chunk_inputs(31, b, n_q, n_kv, d, lens, C, "bf16")
+    for fmt in FORMATS:
+        P = R.MxProblem(inp, fmt, paged=paged, kv_budget=max(lens) // 2)
+        rows = max(lens) + C
+        k, v = (torch.zeros(b, n_kv, rows, d, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+        api.quoka_read_kv_mx(P.p, P.mx, P.k, P.v, 0, rows, k, v, P.ws)
+        out = torch.empty_like(P.out)
+        p = api.make_params(P.q, k, out, P.ctx_len, n_retain=16, kv_budget=max(lens) // 2, max_ctx_len=P.max_ctx)
+        ws = api.alloc_workspace(p)
+        if use_list:
+            k_idx, k_cnt = P.listed(3)
+            api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, P.out, None, P.ws)
+            api.quoka_sparse_attn(p, P.q, k, v, k_idx, k_cnt, out, None, ws)
+        else:
+            api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, P.out, None, P.ws)
+            api.quoka_dense_chunk_attn(p, P.q, k, v, out, None, ws)
+        # one bf16 spacing of the output, and the fp32 sums' last bits where they nearly cancel
+        diff = (P.out.float() - out.float()).abs()
+        assert (diff <= out.float().abs() * 2.0 ** -7 + 1e-4).all(), float(diff.max())
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_a_workspace_of_the_longest_chunk_serves_the_last_one(fmt):
+    inp = synth.make_chunk_inputs(33, 1, 8, 2, 128, [1500], 512, "bf16")
+    P = R.MxProblem(inp, fmt, kv_budget=200)
+    short = synth.make_chunk_inputs(34, 1, 8, 2, 128, [1500], 3, "bf16")
+    S = R.MxProblem(short, fmt, kv_budget=200)
+    assert P.ws.numel() >= S.ws.numel()
+    want = []
+    for ws in (S.ws, P.ws):
+        api.quoka_dense_chunk_attn_mx(S.p, S.mx, S.q, S.k, S.v, S.out, None, ws)
+        want.append(S.out.clone())
+    assert torch.equal(*want)
+    with pytest.raises(api.QuokaError) as e:
+        api.quoka_dense_chunk_attn_mx(S.p, S.mx, S.q, S.k, S.v, S.out, None, S.ws[: api.quoka_workspace_size(S.p)])
+    assert e.value.status == api.ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_empty_batches_entries_and_many_sequences(fmt):
+    """More sequences than a warp has lanes, empty caches among them; generation steps and scores."""
+    lens = [(37 * i) % 300 if i % 5 else 0 for i in range(45)]
+    inp = synth.make_chunk_inputs(35, 45, 4, 2, 64, lens, 1, "bf16")
+    P = R.MxProblem(inp, fmt, paged=True, kv_budget=20, n_retain=4)
+    scores = torch.full((45, 2, P.max_ctx), 7.0, device="cuda")
+    qbar = torch.nn.functional.normalize(torch.randn(45, 2, 1, 64, generator=torch.Generator().manual_seed(1)), dim=-1).bfloat16()
+    api.quoka_score_keys_mx(P.p, P.mx, qbar.cuda(), P.k, scores, P.ws)
+    k_idx, k_cnt = P.listed(5)
+    dense = torch.empty_like(P.out)
+    api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, P.out, None, P.ws)
+    api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, dense, None, P.ws)
+    torch.cuda.synchronize()
+    assert api.quoka_last_device_status(P.ws) == 0
+    for s, T in enumerate(lens):
+        assert (scores[s, :, T:] == 7.0).all()
+        if T:
+            want = O.score_keys(qbar[s].double().numpy(), P.k64[s, :, :T], T)
+            assert np.abs(PA.f64(scores[s, :, :T]) - want).max() <= PA.SCORE_ATOL
+        PA.check_attention(PA.f64(P.out[s]), P.reference(s, use_list=True)[0], "bf16")
+        PA.check_attention(PA.f64(dense[s]), P.reference(s)[0], "bf16")
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("C", [1, 4, 70])
+def test_wide_ranges_of_scales(fmt, C):
+    """Rows and blocks of very different magnitudes, queries with one large element: nothing of the operands' range shows."""
+    inp = synth.make_chunk_inputs(36, 1, 4, 1, 128, [600], C, "bf16")
+    r = np.random.default_rng(4)
+    for x, lo, hi in ((inp.k, -14, 3), (inp.v, -30, 10)):
+        e = torch.from_numpy(r.integers(lo, hi, (1, 1, x.shape[2], 4)).astype(np.float64)).repeat_interleave(32, -1)
+        x.copy_((x.double() * 2.0 ** e).bfloat16())
+    inp.q[..., 5] *= 64
+    P = R.MxProblem(inp, fmt, kv_budget=100)
+    api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, P.out, P.lse, P.ws)
+    out, lse = P.reference(0)
+    got = PA.f64(P.out[0])
+    # weights and outputs in bf16 (fp16 weights in short chunks): half a spacing of the output and 2^-8 of the weighted magnitudes
+    bound = 2.0 ** -8 * np.abs(out) + 2.0 ** -8 * np.abs(P.v64[0, 0, : 600 + C]).max(0)
+    assert (np.abs(got - out) <= bound).all()
+    # logits up to some hundreds: the sums of 128 products and the exponent's scaling in fp32
+    assert np.abs(PA.f64(P.lse[0]) - lse).max() <= 2e-3 + 2.0 ** -18 * np.abs(lse).max()
+
+
 @pytest.mark.parametrize("impl", IMPLS)
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("paged,C,n_retain,budget", [(True, 96, 24, 100), (False, 1, 8, 40), (True, 130, 200, 64), (True, 3, 2, 33)])
