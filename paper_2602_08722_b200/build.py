@@ -16,7 +16,7 @@ LIB = os.path.join(PKG, "libquoka.so")
 LIB_DEBUG = os.path.join(PKG, "libquoka_debug.so")
 SOURCES = ["quoka_api.cu", "select_queries.cu", "score_keys_simt.cu", "score_keys_tc.cu", "select_keys.cu",
            "attn_simt.cu", "attn_f32.cu", "attn_tc.cu", "attn_tc_pair.cu", "no_alloc.cu", "cache_ops.cu", "diagnostics.cu", "decode.cu", "decode_select.cu",
-           "mx_cache.cu", "mx_simt.cu", "mx_api.cu", "attn_tc_mx.cu", "attn_tc_mx8.cu", "attn_tc_mx4.cu", "decode_mx.cu", "score_few_mx.cu"]
+           "mx_cache.cu", "mx_simt.cu", "mx_api.cu", "attn_tc_mx.cu", "attn_tc_mx8.cu", "attn_tc_mx4.cu", "decode_mx.cu", "score_few_mx.cu", "mx_unpack.cu"]
 
 
 def _sources():

@@ -30,7 +30,7 @@
 namespace quoka {
 
 template <int D, int FMT = 0>
-constexpr int kSlotsOf = D == 64 ? 8 : FMT == 0 ? 5 : 4;     // of 16 KB, 32 KB
+constexpr int kSlotsOf = D == 64 ? 8 : kIsMx<FMT> ? 4 : 5;     // of 16 KB, 32 KB
 template <int D, int FMT>
 constexpr int kMxStagesOf = D == 64 ? 4 : FMT == QUOKA_KV_MXFP8 ? 2 : 3;      // raw items of 16 KB beside four slots, or smaller ones
 template <int D, int FMT, bool SPARSE>
@@ -38,18 +38,18 @@ using MxTileLoader = MxLoader<FMT, D, 128, D, SPARSE, kSlotsOf<D, FMT>, kMxStage
 template <int D, int FMT = 0>
 constexpr size_t attn_tc_smem() {
   size_t n = 1024 + (size_t)(2 + kSlotsOf<D, FMT>) * (D / 64) * 16384 + 512;
-  if constexpr (FMT != 0) n += MxTileLoader<D, FMT, false>::kBytes;
+  if constexpr (kIsMx<FMT>) n += MxTileLoader<D, FMT, false>::kBytes;
   return n;
 }
 
 template <int D, bool SPARSE, bool SPLIT, int FMT = 0>
-__global__ void __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1)
+__global__ void __launch_bounds__(kIsMx<FMT> ? kMxAttnThreads : kAttnThreads, 1)
 attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k,
                const __grid_constant__ CUtensorMap tm_v, const __nv_bfloat16* __restrict__ kc,
                const __nv_bfloat16* __restrict__ vc, const int32_t* __restrict__ k_idx,
                const int32_t* __restrict__ k_cnt, __nv_bfloat16* __restrict__ out, float* __restrict__ lse) {
   constexpr int kSlots = kSlotsOf<D, FMT>, HALVES = D / 64;
-  constexpr bool MX = FMT != 0;                              // a microscaled cache: kc, vc are its bytes
+  constexpr bool MX = kIsMx<FMT>;                              // a microscaled cache: kc, vc are its bytes
   constexpr int kThreads = MX ? kMxAttnThreads : kAttnThreads;
   constexpr uint32_t kHalfBytes = 128 * 128;                 // 128 rows x 128 B
   constexpr uint32_t kTileBytes = HALVES * kHalfBytes;       // one Q / K / V tile
@@ -114,6 +114,7 @@ attn_tc_kernel(DevParams P, const __grid_constant__ CUtensorMap tm_q, const __gr
     }
     fence_mbar_init();
   }
+  if constexpr (FMT == kUnpacked) attn_load_nan<D>(P, v_nan, s, kv, g.T + P.chunk);
   if (warp == kQkWarp) tmem_alloc(tmem_slot, 512);
   zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
   tc_fence_before();

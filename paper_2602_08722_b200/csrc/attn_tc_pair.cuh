@@ -49,7 +49,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
                   float* __restrict__ lse) {
   constexpr bool SPLIT = MODE != kWhole;
   constexpr int D = 128;
-  constexpr bool MX = FMT != 0;                               // a microscaled cache: kc, vc are its bytes
+  constexpr bool MX = kIsMx<FMT>;                               // a microscaled cache: kc, vc are its bytes
   constexpr int kThreads = MX ? kMxAttnThreads : kAttnThreads;
   constexpr uint32_t S_COL = 0, P_COL = 128, O_COL = 256;     // Q tile B's P and O are 64 and 128 columns on
   extern __shared__ unsigned char smem_raw[];
@@ -111,6 +111,7 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
     }
     fence_mbar_init();
   }
+  if constexpr (FMT == kUnpacked) attn_load_nan<D>(P, v_nan, s, kv, g.T + P.chunk);
   if (warp == kQkWarp) tmem_alloc_pair(tmem_slot, 512);
   zero_spare_q_rows<D>(P, q_smem, threadIdx.x, kThreads);
   tc_fence_before();
@@ -430,12 +431,12 @@ attn_tc_pair_body(const DevParams& P, const CUtensorMap& tm_q, const CUtensorMap
       const __grid_constant__ CUtensorMap tm_v, const __nv_bfloat16 *__restrict__ kc, const __nv_bfloat16 *__restrict__ vc, \
       const int32_t *__restrict__ k_idx, const int32_t *__restrict__ k_cnt, __nv_bfloat16 *__restrict__ out, float *__restrict__ lse
 template <bool SPARSE, bool SPLIT, int FMT = 0>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_kernel(QUOKA_PAIR_PARAMS) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kIsMx<FMT> ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_kernel(QUOKA_PAIR_PARAMS) {
   attn_tc_pair_body<SPARSE, SPLIT ? kParts : kWhole, FMT>(P, tm_q, tm_k, tm_v, kc, vc, k_idx, k_cnt, out, lse);
 }
 // clusters of (2, parts): the pairs of a row block's parts
 template <bool SPARSE, int FMT = 0>
-__global__ void __launch_bounds__(FMT != 0 ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_cluster_kernel(QUOKA_PAIR_PARAMS) {
+__global__ void __launch_bounds__(kIsMx<FMT> ? kMxAttnThreads : kAttnThreads, 1) attn_tc_pair_cluster_kernel(QUOKA_PAIR_PARAMS) {
   attn_tc_pair_body<SPARSE, kPartsCluster, FMT>(P, tm_q, tm_k, tm_v, kc, vc, k_idx, k_cnt, out, lse);
 }
 
@@ -449,7 +450,7 @@ AttnKernel pick_attn_tc_pair(bool sparse, bool parts, bool in_cluster) {
 template <int FMT>
 size_t attn_tc_pair_smem(const AttnPlan& plan) {
   size_t n = 1024 + 2 * kPairQTileBytes + (size_t)kPairSlots * kPairSlotBytes + 512 + (plan.in_cluster ? 2048 : 0);
-  if constexpr (FMT != 0) n += MxPairLoader<FMT, false>::kBytes;
+  if constexpr (kIsMx<FMT>) n += MxPairLoader<FMT, false>::kBytes;
   return n;
 }
 

@@ -2,6 +2,7 @@
 // the rows a tile holds, the causal limit, and small softmax helpers.
 #pragma once
 
+#include "mx.cuh"
 #include "sm100_ptx.cuh"
 #include "tensor_kernels.cuh"
 
@@ -453,14 +454,27 @@ __device__ __forceinline__ void attn_issue_pv(AttnGeom& g, int t_lo, Resolve&& r
 
 // Epilogue of a softmax thread: its row of O from tensor memory, divided by l, to global memory as bf16 (and the
 // row's log-sum-exp when asked for).
-// FMT: over a microscaled cache of that format (0: bf16).  O is that of values times 2^-16 and has its columns in the order of
-// mx_place, and v_nan has, per 32 columns, the first chunk position that sees a value that is not finite (attn_mx_loader.cuh).
+// FMT: format of the cache (mx.cuh).  Over a microscaled one O is that of values times 2^-16 and has its columns in the order of
+// mx_place; over it, or rows unpacked from it, v_nan has, per 32 columns, the first chunk position that sees a value that is not finite (attn_mx_loader.cuh).
 template <int FMT>
 __device__ __forceinline__ constexpr int mx_place(int e) {
   return FMT == QUOKA_KV_MXFP8 ? (e & ~3) | (e & 1) << 1 | (e & 2) >> 1 : FMT == QUOKA_KV_MXFP4 ? (e & ~7) | (e & 3) << 1 | (e & 4) >> 2 : e;
 }
+// Rows unpacked from a microscaled cache: v_nan from what the unpacking kernel left for the `rows` rows of (s, kv); the whole CTA, with a
+// barrier behind it.
+template <int D>
+__device__ __forceinline__ void attn_load_nan(const DevParams& P, int* v_nan, int s, int kv, int rows) {
+  if (threadIdx.x < D / kMxBlock) v_nan[threadIdx.x] = kNoNan;
+  __syncthreads();
+  const int tiles = (rows + P.v_nan_rows - 1) / P.v_nan_rows;
+  const int32_t* from = P.v_nan + ((size_t)s * P.n_kv + kv) * P.v_nan_tiles * (D / kMxBlock);
+  for (int i = threadIdx.x; i < tiles * (D / kMxBlock); i += blockDim.x) {
+    const int at = __ldcg(from + i);
+    if (at != kNoNan) atomicMin(v_nan + i % (D / kMxBlock), at);
+  }
+}
 template <int FMT>
-__device__ __forceinline__ float attn_inverse(float l) { return FMT != 0 ? 65536.f / l : 1.f / l; }
+__device__ __forceinline__ float attn_inverse(float l) { return kIsMx<FMT> ? 65536.f / l : 1.f / l; }
 template <int FMT>
 __device__ __forceinline__ void attn_mark_nan(uint32_t (&r)[32], const int* v_nan, int c, int row) {
   if constexpr (FMT != 0) {

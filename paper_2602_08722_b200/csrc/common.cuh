@@ -36,6 +36,10 @@ struct DevParams {
   int64_t kv_rows;  // rows per (sequence, head) when contiguous
   const uint8_t* k_scale;   // scale bytes of a microscaled cache (mx.cuh), else null
   const uint8_t* v_scale;
+  // attention over rows unpacked from one (mx_unpack.cu): per (sequence, KV head) and `v_nan_rows` rows, the first chunk position that
+  // sees a value that is not finite, of each 32 columns; v_nan_tiles of them per (sequence, KV head)
+  const int32_t* v_nan;
+  int v_nan_rows, v_nan_tiles;
   // split attention (small grids): room for the parts' partial results and their arrival counters, or null
   float* attn_partials;
   int32_t* attn_counters;

@@ -14,6 +14,11 @@ constexpr int kMxBlock = 32;
 constexpr int kMxExpMin = -64, kMxExpMax = 15;    // exponents of a scale, as quoka_append_kv_mx writes them
 constexpr uint32_t kMxNanScale = 255;             // a block with a value that is not finite reads back as NaN
 
+constexpr int kNoNan = 0x7FFFFFFF;                   // no position, or key, that sees a value that is not finite
+// Formats of a cache that an attention kernel is made for: 0 bf16, QUOKA_KV_MXFP8, QUOKA_KV_MXFP4, and bf16 rows unpacked from either.
+constexpr int kUnpacked = 3;
+template <int FMT>
+constexpr bool kIsMx = FMT == QUOKA_KV_MXFP8 || FMT == QUOKA_KV_MXFP4;
 template <int FMT>
 constexpr int kMxBits = FMT == QUOKA_KV_MXFP8 ? 8 : 4;
 

@@ -39,33 +39,50 @@ static quoka_status run_score_keys_mx(const quoka_params* p, const quoka_mx_cach
   return QUOKA_OK;
 }
 
-static quoka_status run_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const DevParams& P, const void* q, const void* k, const void* v,
-                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, const AttnPlan& plan,
-                                bool after_selection = false) {
-  if (p->impl == QUOKA_IMPL_AUTO && attn_mx_tc_supported(p) && decode_mx_applies(p)) {
-    QUOKA_TRY_CUDA(launch_decode_mx(P, mx->format, q, k, v, k_idx, k_cnt, out, lse, P.attn_partials, st, after_selection));
-    return QUOKA_OK;
-  }
-  if (p->impl != QUOKA_IMPL_SIMT && attn_mx_tc_supported(p))
-    return launch_attn_mx_tc(p, P, mx->format, q, k, v, k_idx, k_cnt, out, lse, st, after_selection, plan);
-  if (p->impl == QUOKA_IMPL_TENSOR) return QUOKA_ERR_UNSUPPORTED;
-  QUOKA_TRY_CUDA(launch_attn_mx_simt(P, p->dtype, mx->format, q, k, v, k_idx, k_cnt, out, lse, st));
-  return QUOKA_OK;
-}
-
-// The scratch of a few query rows' attention comes last and has to be there.
+// The scratch of a few query rows' attention comes last and has to be there; that of unpacked rows comes last too and may be missing.
 static size_t scratch_mx(const quoka_params* p) { return p->dtype == QUOKA_BF16 && decode_mx_applies(p) ? decode_mx_scratch_bytes(p) : 0; }
 static quoka_status check_ws_mx(const quoka_params* p, void* ws, size_t ws_bytes) {
   const quoka_status st = check_ws(p, ws, ws_bytes);
   if (st != QUOKA_OK) return st;
   return ws_bytes < workspace_bytes_unsplit(p) + scratch_mx(p) ? QUOKA_ERR_WORKSPACE : QUOKA_OK;
 }
-// The buffers of an attention call that follows `plan`.
-static Workspace carve_mx(const quoka_params* p, void* ws, size_t ws_bytes, const AttnPlan& plan) {
-  if (scratch_mx(p) == 0) return carve(p, ws, ws_bytes, &plan);
-  Workspace w = carve(p, ws);
-  w.attn_partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + w.total);
-  return w;
+
+// How an attention call is done: its plan, buffers, and scratch of unpacked rows.
+struct MxAttn {
+  AttnPlan plan;
+  Workspace w;
+  void* unpacked = nullptr;
+};
+static MxAttn plan_attn_mx(const quoka_params* p, void* ws, size_t ws_bytes, bool listed) {
+  MxAttn a;
+  const auto plan = [&](size_t room) { return listed ? attn_plan_sparse(p, budget_cap_of(p), room) : attn_plan_dense(p, room); };
+  if (scratch_mx(p) > 0) {
+    a.plan = plan(0);
+    a.w = carve(p, ws);
+    a.w.attn_partials = reinterpret_cast<float*>(static_cast<unsigned char*>(ws) + a.w.total);
+    return a;
+  }
+  const size_t room = attn_room(p, ws_bytes), unpack = attn_mx_tc_supported(p) ? attn_unpack_bytes(p, listed) : 0;
+  const bool unpacks = unpack > 0 && unpack <= room;
+  a.plan = plan(unpacks ? room - unpack : room);
+  a.w = carve(p, ws, unpacks ? ws_bytes - unpack : ws_bytes, &a.plan);
+  if (unpacks) a.unpacked = static_cast<unsigned char*>(ws) + a.w.total;
+  return a;
+}
+
+static quoka_status run_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const DevParams& P, const MxAttn& a, const void* q, const void* k,
+                                const void* v, const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st,
+                                bool after_selection = false) {
+  if (p->impl == QUOKA_IMPL_AUTO && attn_mx_tc_supported(p) && decode_mx_applies(p)) {
+    QUOKA_TRY_CUDA(launch_decode_mx(P, mx->format, q, k, v, k_idx, k_cnt, out, lse, P.attn_partials, st, after_selection));
+    return QUOKA_OK;
+  }
+  if (a.unpacked) return launch_attn_mx_unpacked(p, P, mx->format, q, k, v, k_idx, k_cnt, out, lse, a.unpacked, st, after_selection, a.plan);
+  if (p->impl != QUOKA_IMPL_SIMT && attn_mx_tc_supported(p))
+    return launch_attn_mx_tc(p, P, mx->format, q, k, v, k_idx, k_cnt, out, lse, st, after_selection, a.plan);
+  if (p->impl == QUOKA_IMPL_TENSOR) return QUOKA_ERR_UNSUPPORTED;
+  QUOKA_TRY_CUDA(launch_attn_mx_simt(P, p->dtype, mx->format, q, k, v, k_idx, k_cnt, out, lse, st));
+  return QUOKA_OK;
 }
 
 }  // namespace quoka
@@ -81,7 +98,8 @@ quoka_status quoka_workspace_size_mx(const quoka_params* p, const quoka_mx_cache
   size_t attn = 0;
   if (quoka_workspace_size(p, &attn) != QUOKA_OK) return QUOKA_ERR_INVALID_ARG;
   // (with the scratch of the shortest chunks, whatever this one's length: the last chunk of a prompt comes with the workspace of its longest)
-  *bytes = std::max(attn, workspace_bytes_unsplit(p) + (p->dtype == QUOKA_BF16 ? decode_mx_scratch_bytes(p) : 0));
+  *bytes = std::max(attn + std::max(attn_unpack_bytes(p, true), attn_unpack_bytes(p, false)),
+                    workspace_bytes_unsplit(p) + (p->dtype == QUOKA_BF16 ? decode_mx_scratch_bytes(p) : 0));
   return QUOKA_OK;
 }
 
@@ -128,9 +146,8 @@ quoka_status quoka_sparse_attn_mx(const quoka_params* p, const quoka_mx_cache* m
   if (!q || !k_cache || !v_cache || !k_idx || !k_cnt || !out) return QUOKA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
-  const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve_mx(p, ws, ws_bytes, plan)), q, k_cache, v_cache, k_idx, k_cnt, out, lse,
-                     static_cast<cudaStream_t>(stream), plan);
+  const MxAttn a = plan_attn_mx(p, ws, ws_bytes, /*listed=*/true);
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, a.w), a, q, k_cache, v_cache, k_idx, k_cnt, out, lse, static_cast<cudaStream_t>(stream));
 }
 
 quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
@@ -140,9 +157,8 @@ quoka_status quoka_dense_chunk_attn_mx(const quoka_params* p, const quoka_mx_cac
   if (!q || !k_cache || !v_cache || !out) return QUOKA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
-  const AttnPlan plan = attn_plan_dense(p, attn_room(p, ws_bytes));
-  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, carve_mx(p, ws, ws_bytes, plan)), q, k_cache, v_cache, nullptr, nullptr, out, lse,
-                     static_cast<cudaStream_t>(stream), plan);
+  const MxAttn a = plan_attn_mx(p, ws, ws_bytes, /*listed=*/false);
+  return run_attn_mx(p, mx, make_dev_mx(p, mx, ws, a.w), a, q, k_cache, v_cache, nullptr, nullptr, out, lse, static_cast<cudaStream_t>(stream));
 }
 
 quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache* mx, const void* q, const void* k_cache, const void* v_cache,
@@ -153,8 +169,8 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
-  const AttnPlan plan = attn_plan_sparse(p, budget_cap_of(p), attn_room(p, ws_bytes));
-  const Workspace w = carve_mx(p, ws, ws_bytes, plan);
+  const MxAttn a = plan_attn_mx(p, ws, ws_bytes, /*listed=*/true);
+  const Workspace& w = a.w;
   const DevParams P = make_dev_mx(p, mx, ws, w);
   int32_t* k_idx = k_idx_out ? k_idx_out : w.k_idx;
   int32_t* k_cnt = k_cnt_out ? k_cnt_out : w.k_cnt;
@@ -166,7 +182,7 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
     QUOKA_TRY_CUDA(cudaMemsetAsync(P.attn_counters, 0, P.n_attn_counters * sizeof(int32_t), cs));
   }
   QUOKA_TRY_CUDA(launch_select_keys(P, w.scores, k_idx, k_cnt, cs, /*chained=*/p->max_ctx_len > 0));
-  return run_attn_mx(p, mx, P, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs, plan, /*after_selection=*/true);
+  return run_attn_mx(p, mx, P, a, q, k_cache, v_cache, k_idx, k_cnt, out, nullptr, cs, /*after_selection=*/true);
 }
 
 }  // extern "C"

@@ -14,7 +14,6 @@ namespace quoka {
 
 constexpr int kMxShift = 16;                         // tiles hold values times 2^-kMxShift
 constexpr float kMxUnshift = 65536.f;
-constexpr int kNoNan = 0x7FFFFFFF;                   // no position, or key, that sees a value that is not finite
 
 // 16 elements of a row.
 template <int FMT> struct MxUnit;

@@ -473,3 +473,45 @@ def test_calls_capture_into_a_graph_and_run_on_another_stream(fmt):
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(P.out, want[0][0]) and torch.equal(dense, want[0][1])
+
+
+# Chunks that are long enough for their rows to be unpacked first: 2048 query rows per KV head, 8192 over a whole cache of 128 columns.
+UNPACKED = [(8, 1, 64, [700, 90], 257, True), (8, 2, 64, [130, 0], 513, False), (16, 1, 64, [333], 300, True), (8, 1, 128, [450, 1], 258, True),
+            (12, 2, 128, [200], 345, False), (16, 1, 128, [600, 77], 513, True), (8, 1, 128, [64], 1025, False)]
+
+
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("n_q,n_kv,d,lens,C,paged", UNPACKED)
+def test_unpacked_chunks_are_the_bf16_call_on_what_the_cache_reads_as(use_list, n_q, n_kv, d, lens, C, paged):
+    test_long_chunks_are_the_bf16_call_on_what_the_cache_reads_as(use_list, n_q, n_kv, d, lens, C, paged)
+
+
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n_q,n_kv,d,T,C,bad_k,bad_v", [
+    # blocks in cached rows, in the chunk, at the edges of an unpacking tile (64 rows of 128 columns, 128 of 64), in the last row
+    (8, 1, 64, 300, 257, [], [(7, 1), (300 + 250, 0)]), (8, 1, 64, 90, 260, [(95, 0)], [(127, 1), (128, 0)]), (8, 1, 128, 190, 260, [], [(191, 3), (192, 2), (449, 0)]),
+    (8, 1, 128, 40, 300, [(339, 1)], [(39, 2)]), (16, 1, 128, 70, 520, [], [(71, 0), (400, 3)]), (8, 1, 128, 0, 1030, [(1000, 1)], [(63, 0), (1029, 2)])])
+def test_blocks_that_are_not_finite_in_unpacked_chunks(use_list, fmt, n_q, n_kv, d, T, C, bad_k, bad_v):
+    test_blocks_that_are_not_finite_reach_only_the_rows_that_see_them(api.IMPL_AUTO, use_list, fmt, 1, n_q, n_kv, d, T, C, bad_k, bad_v)
+
+
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d,n_q,C", [(64, 8, 300), (128, 16, 530)])
+def test_chunks_convert_where_the_workspace_has_no_room_for_unpacked_rows(use_list, fmt, d, n_q, C):
+    """quoka_workspace_size's bytes are enough; one byte less than what unpacking takes is too, and nothing behind them is written."""
+    inp = synth.make_chunk_inputs(35, 2, n_q, 1, d, [400, 129], C, "bf16")
+    P = R.MxProblem(inp, fmt, kv_budget=100, paged=True)
+    least, full = api.quoka_workspace_size(P.p), P.ws.numel()
+    assert least < full
+    args = P.listed(5) if use_list else ()
+    call = api.quoka_sparse_attn_mx if use_list else api.quoka_dense_chunk_attn_mx
+    for n in (full, full - 1, least):
+        ws = torch.full((full + 256,), 0xA5, dtype=torch.uint8, device="cuda")
+        P.out.fill_(7.0)
+        call(P.p, P.mx, P.q, P.k, P.v, *args, P.out, P.lse, ws[:n])
+        assert (ws[n:] == 0xA5).all()
+        for s in range(2):
+            want, _ = P.reference(s, use_list=use_list)
+            assert (np.abs(PA.f64(P.out[s]) - want) <= PA.attention_bound(want, "bf16")).all()
