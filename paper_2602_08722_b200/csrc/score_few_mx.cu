@@ -47,7 +47,11 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
   int pos = in.begin + warp;
   bool more = true;
   const auto fill = [&](int stage) {
-    while (more && pos >= in.end) { more = in.next(P, work); pos = in.begin + warp; }
+    while (more && pos >= in.end) {                   // (the warps take granules of the share in turn, across its parts)
+      const int past = pos - in.end;
+      more = in.next(P, work);
+      pos = in.begin + past;
+    }
     if (more) {
       const int first = pos * kDecGranule, t = first + lane < in.lens.cnt ? first + lane : -1;
       uint32_t place, srow;
@@ -87,10 +91,16 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
   grid_dependency_wait();                             // Q-bar comes from the kernel before
   uint32_t qf[2 * KSTEPS];
   float qs[2] = {0.f, 0.f};
-  int stage = 0, s_cur = -1, kv_cur = -1;
+  int stage = 0, s_cur = -1, kv_cur = -1, gr = part.begin + warp;
   uint32_t phase = 0;
   bool ok = true;
-  for (bool again = true; again && ok; again = part.next(P, work)) {
+  for (bool again = true; again && ok;) {
+    if (gr >= part.end) {
+      const int past = gr - part.end;
+      again = part.next(P, work);
+      gr = part.begin + past;
+      continue;
+    }
     if (part.s != s_cur || part.kv != kv_cur) {       // queries past the retained ones are zeros
       s_cur = part.s; kv_cur = part.kv;
       const __nv_bfloat16* qr = qbar + (((long long)part.s * P.n_kv + part.kv) * P.n_sel + min(g, P.n_sel - 1)) * D;
@@ -120,7 +130,7 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
     }
     float* out = scores + ((long long)part.s * P.n_kv + part.kv) * P.max_ctx;
 #pragma unroll 1
-    for (int gr = part.begin + warp; gr < part.end; gr += WARPS) {
+    for (; gr < part.end; gr += WARPS) {
       cp_async_wait<ST - 1>();
       if (!mbar_wait_done(&landed[stage], phase, wc)) { ok = false; break; }
       __syncwarp();
@@ -211,7 +221,7 @@ cudaError_t launch_score_few_mx(const DevParams& P, int fmt, const void* qbar, c
   const int sms = device_sm_count();
   if (sms <= 0) return cudaErrorInvalidDevice;
   const long long granules = (long long)P.batch * P.n_kv * ((P.max_ctx + kDecGranule - 1) / kDecGranule);
-  const long long ctas = std::min<long long>(sms, (granules + kFewWarps - 1) / kFewWarps);
+  const long long ctas = std::min<long long>(sms, granules);
   const DecWork work{1, 0, nullptr};
   const cudaError_t e = mx_dispatch(QUOKA_BF16, fmt, P.d, [&](auto, auto f, auto d) {
     constexpr int FMT = decltype(f)::value, D = decltype(d)::value;
