@@ -18,12 +18,18 @@
 //   P  weights 2^(x - m), m a reference point that the largest exponent x exceeds by 7 when it is set and by 15 at most: weights below 2^-25, against a largest one of
 //      2^7 or more, vanish (a hundred thousand of them are 2^-15 of the sum).
 //
-// Split: the 32-key granules of all (sequence, KV head, row group) in one list, cut into equal contiguous shares, one per CTA; inside a
-// CTA the warps take granules in turn, each with a running maximum, sum and output of its own, added up at the end of a unit's part.
-// A unit that several CTAs share is added up by a second kernel, part by part in order.  Long lists are balanced whatever the
-// sequences' lengths are.  Weights are rounded to fp16 for the product and divided by their sum as rounded, so that they add up to
+// Split: units are (sequence, KV head, row group).  Few keys: a CTA per unit, or a cluster of CTAs with an equal share of the unit's granules of
+// 32 keys each, whose results are added up through distributed shared memory.  Else the granules of all units are one list, cut into equal contiguous
+// shares, one per CTA, and a second kernel adds up the units that several CTAs share: long lists are balanced whatever the sequences' lengths
+// are.  Inside a CTA the warps take granules in turn, each with a running maximum, sum and output of its own, added up at the end of a unit's part.
+// All parts are added up in order.  Weights are rounded to fp16 for the product and divided by their sum as rounded, so that they add up to
 // one; the log-sum-exp is that of the weights before.
+//
+// Measured, MXFP8 / MXFP4, us: 16 sequences of 8192 to 32768 rows, 8 KV heads of 4, d 128, one position: 132 / 128 (735 MB of MXFP8: 5.6 TB/s;
+// over a bf16 cache 557); one of 131072 rows 63 / 59, of 32768 29 / 27, of 4003 14.4.  The main kernel over 131072 rows: 867 instructions per 32 keys,
+// the issue ports busy for 48 % of the cycles, the integer pipe for 47 %.
 #include <algorithm>
+#include <atomic>
 
 #include "decode_mx.cuh"
 
@@ -33,12 +39,13 @@ namespace quoka {
 // are added up, which halves the shared memory for it: twelve rings of 8-bit rows leave 29 KB.
 template <int NT>
 constexpr int kDecWarps = NT == 1 ? 12 : 8;
+constexpr int kDecAtOnce = 8;                          // parts of a cluster whose results a thread has on their way
 template <int NT>
 constexpr int kDecLast = NT == 1 ? 6 : 8;
 template <int FMT, int D, int NT>
 __global__ void __launch_bounds__(32 * kDecWarps<NT>, 1)
 decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q, const uint8_t* __restrict__ kc, const uint8_t* __restrict__ vc,
-                 const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int whole_units,
+                 const int32_t* __restrict__ k_idx, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, float* __restrict__ parts, int per_unit,
                  const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v) {
   typedef DecBytes<FMT, D> B;
   constexpr int WARPS = kDecWarps<NT>, LAST = kDecLast<NT>, ST = kDecStages, ROWS = 8 * NT, TILES = D / 16, KSTEPS = D / 16;
@@ -58,14 +65,20 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   const WaitCtx wc{&abort_flag, P.status};
   // ---- this CTA's share
   const auto share = [&]() -> DecPart {
-    if (whole_units) return DecPart(P, work, blockIdx.x);
+    if (per_unit > 0) {
+      DecPart p(P, work, blockIdx.x / per_unit);
+      const int rank = blockIdx.x % per_unit;
+      p.begin = (int)((long long)p.n * rank / per_unit);
+      p.end = (int)((long long)p.n * (rank + 1) / per_unit);
+      return p;
+    }
     const DecTotals all(P, work, 0, lane);
     const long long each = all.share(gridDim.x), lo = min(each * blockIdx.x, all.total);
     if (lo == all.total) { DecPart none(P, work, 0); none.end = 0; return none; }
     return DecPart(P, work, all, lo, min(lo + each, all.total), lane);
   };
   DecPart in = share();
-  if (in.begin >= in.end) return;                     // (nothing of the list is left for this CTA)
+  if (in.begin >= in.end && per_unit <= 1) return;    // (nothing of the list is left for this CTA)
   DecPart part = in;
   if (threadIdx.x == 0) abort_flag = 0;
   if (lane == 0) {
@@ -462,7 +475,15 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         }
     }
     __syncthreads();
-    const bool is_whole = part.begin == 0 && part.end == part.n;
+    const auto store = [&](int row, int col, const float4& acc, float mx, float sum, float sumx) {
+      const int r = first_row + row, h = part.kv * P.group + r % P.group, pos_r = r / P.group;
+      const float inv = 1.f / sum;
+      const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), b = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
+      *reinterpret_cast<uint2*>(out + (long long)part.s * P.o_sb + (long long)h * P.o_sh + (long long)pos_r * P.o_st + col) =
+          make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
+      if (lse && col == 0) lse[((long long)part.s * P.n_q + h) * P.chunk + pos_r] = (mx + log2f(sumx)) * 0.6931471805599453f;
+    };
+    const bool is_whole = per_unit <= 1 && part.begin == 0 && part.end == part.n;
     const int slot = blockIdx.x * 2 + (part.begin == 0 ? 1 : 0);
     for (int i = threadIdx.x; i < n_rows * (D / 4); i += 32 * WARPS) {
       const int row = i / (D / 4), col = i % (D / 4) * 4;
@@ -480,17 +501,46 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         acc.x = fmaf(wt, v.x, acc.x); acc.y = fmaf(wt, v.y, acc.y); acc.z = fmaf(wt, v.z, acc.z); acc.w = fmaf(wt, v.w, acc.w);
       }
       if (is_whole) {
-        const int r = first_row + row, h = part.kv * P.group + r % P.group, pos_r = r / P.group;
-        const float inv = 1.f / sum;
-        const __nv_bfloat162 a = __floats2bfloat162_rn(acc.x * inv, acc.y * inv), b = __floats2bfloat162_rn(acc.z * inv, acc.w * inv);
-        *reinterpret_cast<uint2*>(out + (long long)part.s * P.o_sb + (long long)h * P.o_sh + (long long)pos_r * P.o_st + col) =
-            make_uint2(*reinterpret_cast<const uint32_t*>(&a), *reinterpret_cast<const uint32_t*>(&b));
-        if (lse && col == 0) lse[((long long)part.s * P.n_q + h) * P.chunk + pos_r] = (mx + log2f(sumx)) * 0.6931471805599453f;
+        store(row, col, acc, mx, sum, sumx);
       } else {
-        float* to = parts + (size_t)slot * ROWS * (D + 3);
+        float* to = per_unit > 1 ? reinterpret_cast<float*>(dec_smem) : parts + (size_t)slot * ROWS * (D + 3);        // (the rings are empty by then)
         *reinterpret_cast<float4*>(to + row * D + col) = acc;
         if (col == 0) { to[ROWS * D + row] = mx; to[ROWS * (D + 1) + row] = sum; to[ROWS * (D + 2) + row] = sumx; }
       }
+    }
+    if (per_unit > 1) {                                // one part: the cluster's are added up, in order, each CTA a share of the outputs
+      cluster_sync_all();
+      const uint32_t mine = smem_u32(dec_smem);
+      const int rank = blockIdx.x % per_unit, items = n_rows * (D / 4);
+      for (int i = rank + per_unit * (int)threadIdx.x; i < items; i += per_unit * 32 * WARPS) {
+        const int row = i / (D / 4), col = i % (D / 4) * 4;
+        float mx = -INFINITY, sum = 0.f, sumx = 0.f;
+        float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 1
+        for (int p0 = 0; p0 < per_unit; p0 += kDecAtOnce) {
+          float pm[kDecAtOnce], pl[kDecAtOnce], plx[kDecAtOnce];
+          float4 v[kDecAtOnce];
+#pragma unroll
+          for (int j = 0; j < kDecAtOnce; ++j) {
+            const uint32_t from = map_to_cta(mine, (uint32_t)min(p0 + j, per_unit - 1));
+            v[j] = ld_cluster_f4(from + 4u * (uint32_t)(row * D + col));
+            pm[j] = ld_cluster_f(from + 4u * (uint32_t)(ROWS * D + row));
+            pl[j] = ld_cluster_f(from + 4u * (uint32_t)(ROWS * (D + 1) + row));
+            plx[j] = ld_cluster_f(from + 4u * (uint32_t)(ROWS * (D + 2) + row));
+          }
+#pragma unroll
+          for (int j = 0; j < kDecAtOnce; ++j)
+            if (p0 + j < per_unit) {
+              const float top = fmaxf(mx, pm[j]), w0 = dec_weight(mx, top), w1 = dec_weight(pm[j], top);
+              mx = top;
+              sum = fmaf(w1, pl[j], sum * w0);
+              sumx = fmaf(w1, plx[j], sumx * w0);
+              acc.x = fmaf(w1, v[j].x, acc.x * w0); acc.y = fmaf(w1, v[j].y, acc.y * w0); acc.z = fmaf(w1, v[j].z, acc.z * w0); acc.w = fmaf(w1, v[j].w, acc.w * w0);
+            }
+        }
+        store(row, col, acc, mx, sum, sumx);
+      }
+      cluster_sync_all();                              // (nobody leaves while its shared memory is read)
     }
     again = part.next(P, work);
   }
@@ -571,7 +621,8 @@ static int dec_tiles(int rows, int d) {
 }
 
 // Query rows that these kernels take: more of them are faster in a 128-row tile of the tensor-core kernel, though it walks 128 keys for every
-// 1.0 to 1.4 us and cuts them into 8 parts at most.
+// 1.0 to 1.4 us and cuts them into 8 parts at most.  These / those, us: d 128, 20 to 32 rows over 32768 keys 46 / 83, over 4003 18.4 / 22.6, over 8 sequences of
+// 8192 80 / 78; d 64, 40 rows over 3 sequences of 20011 42 / 45, 64 rows 64 / 44.
 bool decode_mx_applies(const quoka_params* p) {
   const long long rows = (long long)p->chunk_len * (p->n_q_heads / p->n_kv_heads);
   return p->chunk_len == 1 || rows <= (p->head_dim == 64 ? 40 : 32);
@@ -581,6 +632,39 @@ bool decode_mx_applies(const quoka_params* p) {
 size_t decode_mx_scratch_bytes(const quoka_params* p) {
   const int sms = device_sm_count() > 0 ? device_sm_count() : 148;
   return (size_t)sms * 2 * (p->head_dim == 64 ? 40 : 16) * (p->head_dim + 3) * sizeof(float);
+}
+
+constexpr int kDecWhole = 24;                          // granules that a CTA takes alone
+// The largest cluster of up to 16 CTAs of which `units` are resident at once (1: none): a property of the device and the kernel, asked for once.
+template <int FMT, int D, int NT>
+static int largest_cluster(long long units, size_t smem) {
+  constexpr int kMost = 16, kDevices = 64;
+  static std::atomic<int> resident[kDevices][kMost + 1];       // + 1
+  int dev = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return 1;
+  for (int cl = (int)std::min<long long>(kMost, device_sm_count() / units); cl > 1; --cl) {
+    int n = resident[dev][cl].load(std::memory_order_relaxed);
+    if (n == 0) {
+      const auto kernel = decode_mx_kernel<FMT, D, NT>;
+      cudaLaunchConfig_t cfg = {};
+      cfg.gridDim = dim3((unsigned)cl);
+      cfg.blockDim = dim3(32 * kDecWarps<NT>);
+      cfg.dynamicSmemBytes = smem;
+      cudaLaunchAttribute attr;
+      attr.id = cudaLaunchAttributeClusterDimension;
+      attr.val.clusterDim.x = (unsigned)cl;
+      attr.val.clusterDim.y = attr.val.clusterDim.z = 1;
+      cfg.attrs = &attr;
+      cfg.numAttrs = 1;
+      if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess || cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+      }
+      resident[dev][cl].store(++n, std::memory_order_relaxed);
+    }
+    if (n > units) return cl;
+  }
+  return 1;
 }
 
 template <int FMT, int D, int NT>
@@ -595,21 +679,32 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   if (sms <= 0) return cudaErrorInvalidDevice;
   const long long units = (long long)P.batch * P.n_kv * work.groups;
   const long long most = ((k_idx ? (long long)P.budget_cap : (long long)P.max_ctx) + P.chunk + kDecGranule - 1) / kDecGranule;      // granules of a unit
-  // A CTA per unit where that is two rounds of its warps or fewer, or where units are many: what joining parts costs (a launch, a
-  // round trip through L2) is more than what the shorter rounds gain.
-  const bool whole = most <= 2 * WARPS || units >= 64ll * sms;
-  const long long ctas = whole ? units : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
-  if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
-  CUtensorMap tm_k, tm_v;
-  if (!encode_mx_tile_map(&tm_k, P, FMT, k, kDecGranule) || !encode_mx_tile_map(&tm_v, P, FMT, v, kDecGranule)) return cudaErrorInvalidValue;
   const size_t smem = 1024 + (size_t)WARPS * kDecStages * (DecBytes<FMT, D>::kStage + 8) + (size_t)kDecLast<NT> * ROWS * (D + 4 + 3) * sizeof(float);
   cudaError_t e = cudaFuncSetAttribute(decode_mx_kernel<FMT, D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
   if (e != cudaSuccess) return e;
-  e = launch_kernel("decode_mx", decode_mx_kernel<FMT, D, NT>, dim3((unsigned)ctas), dim3(32 * WARPS), smem, st, 1, chained, P, work, (const __nv_bfloat16*)q,
-                    (const uint8_t*)k, (const uint8_t*)v, k_idx, (__nv_bfloat16*)out, lse, parts, whole ? 1 : 0, tm_k, tm_v);
+  // How units are shared, us of one sequence, 8 KV heads, d 128, one position of 4 heads, MXFP8, over 300 / 700 / 1000 / 1500 / 2000 / 4003 / 8192 / 16384 / 32768 rows:
+  //   a CTA per unit       9.0 / 12.3 / 12.8 / 16.4 / 18.5
+  //   a cluster per unit   1000 rows on: 12.3 / 12.3 / 12.3 / 14.4 / 16.4 / 20.5 / 28.7 (of 10 CTAs: on a B200 seven clusters of 11 to 16 are resident, 11 of 10)
+  //   one list             16.4 to 4003 rows / 20.5 / 22.9 / 28.7: joining parts costs a launch and a round trip through L2, some 3 rounds of the warps
+  // so a CTA to 24 granules (four positions over 700 rows: 14.4 alone, 16.4 in clusters), then clusters where they take 3 rounds more than the list at
+  // most.  Sequences of a batch may differ, and their clusters do not help each other: 4 rounds at most.  (8 sequences of 1500 rows: 14.4, as a list 20.5.)
+  // No clusters: a CTA to 4 rounds (the same 8 sequences 16.4), or where units are many.
+  int per_unit = most <= kDecWhole || units >= 64ll * sms ? 1 : 0;
+  if (per_unit == 0) {
+    const int cl = largest_cluster<FMT, D, NT>(units, smem);
+    const auto rounds = [&](long long granules, long long over) { return (granules + over * WARPS - 1) / (over * WARPS); };
+    if (cl > 1 && rounds(most, cl) <= 3 + (P.batch == 1 ? rounds(units * most, sms) : 1)) per_unit = cl;
+    else if (most <= 4 * WARPS) per_unit = 1;
+  }
+  const long long ctas = per_unit > 0 ? units * per_unit : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
+  if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidConfiguration;
+  CUtensorMap tm_k, tm_v;
+  if (!encode_mx_tile_map(&tm_k, P, FMT, k, kDecGranule) || !encode_mx_tile_map(&tm_v, P, FMT, v, kDecGranule)) return cudaErrorInvalidValue;
+  e = launch_kernel("decode_mx", decode_mx_kernel<FMT, D, NT>, dim3((unsigned)ctas), dim3(32 * WARPS), smem, st, std::max(per_unit, 1), chained, P, work, (const __nv_bfloat16*)q,
+                    (const uint8_t*)k, (const uint8_t*)v, k_idx, (__nv_bfloat16*)out, lse, parts, per_unit, tm_k, tm_v);
   if (e != cudaSuccess) return e;
   count_launch();
-  if (!whole) {
+  if (per_unit == 0) {
     e = launch_kernel("decode_mx_join", decode_mx_join_kernel<D, NT>, dim3((unsigned)units, ROWS), dim3(32 * kJoinWarps), 0, st, 1, true, P, work, (const float*)parts, (int)ctas,
                       (__nv_bfloat16*)out, lse);
     if (e != cudaSuccess) return e;

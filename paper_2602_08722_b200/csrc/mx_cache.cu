@@ -5,7 +5,7 @@
 //   the conversion instruction.  The inverse norm of a key row is that of the values the cache then holds.
 // read: cache rows first .. first + n - 1 to dense [b][n_KV][n][D] tensors; rows at and beyond T_s + C are left as they were.
 //   A lane turns 8 elements of K and of V into 16 (bf16) or 32 bytes (f32).
-// Both are bound by HBM; a generation step's rows by the launch.
+// Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 101 us, 5.5 TB/s of 0.56 GB); a generation step's rows by the launch.
 #include "mx.cuh"
 #include "mx_host.cuh"
 
@@ -167,7 +167,8 @@ __global__ void __launch_bounds__(kMxThreads) read_kv_mx_kernel(DevParams P, con
 }
 
 // ---------------------------------------------------------------------------------------------- host
-// Rows per thread: four where the CTAs then still make two waves, else one.
+// Rows per thread: four where the CTAs then still make two waves, else one.  One / four, us, 8 KV heads, d 128, MXFP8: append of 8 times 4096 rows 41.0 / 36.7,
+// 16 of one row 7.2 / 7.4, read of 8192 rows 13.1 / 9.4, of 2000 rows 5.9 / 6.1, of 4 sequences of 20011 to 32768 rows 162 / 112 (MXFP4 161 / 101).
 struct MxGrid { int unr, tiles; int64_t ctas; };
 static MxGrid mx_grid(const DevParams& P, int64_t rows) {
   const int64_t units = (int64_t)P.batch * P.n_kv;

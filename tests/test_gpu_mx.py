@@ -515,3 +515,26 @@ def test_chunks_convert_where_the_workspace_has_no_room_for_unpacked_rows(use_li
         for s in range(2):
             want, _ = P.reference(s, use_list=use_list)
             assert (np.abs(PA.f64(P.out[s]) - want) <= PA.attention_bound(want, "bf16")).all()
+
+
+@pytest.mark.parametrize("use_list", [False, True])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n_q,n_kv,d,lens,C,paged", [
+    # units that a cluster shares: sequences with fewer granules of 32 keys than the cluster has CTAs, of no keys, one granule more than a CTA takes
+    (8, 2, 128, [1700, 0, 33], 1, True), (4, 1, 128, [780], 1, False), (8, 1, 128, [3000, 5], 2, True), (4, 1, 64, [5000, 31, 64], 3, False), (8, 1, 64, [2100, 1], 3, True),
+    (16, 2, 64, [1300, 0], 5, False), (32, 8, 128, [4003], 1, True), (32, 8, 128, [1500, 40], 4, False), (5, 5, 64, [1025, 1024, 7], 1, True)])
+def test_few_rows_shared_in_clusters(use_list, fmt, n_q, n_kv, d, lens, C, paged):
+    inp = synth.make_chunk_inputs(41, len(lens), n_q, n_kv, d, lens, C, "bf16")
+    P = R.MxProblem(inp, fmt, paged=paged, kv_budget=max(lens) - 1)
+    for _ in range(2):                                        # (the same bits every time)
+        if use_list:
+            k_idx, k_cnt = P.listed(3)
+            api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, P.out, P.lse, P.ws)
+        else:
+            api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, P.out, P.lse, P.ws)
+        first = P.out.clone() if _ == 0 else first
+    assert torch.equal(first, P.out)
+    for s in range(len(lens)):
+        want, lse = P.reference(s, use_list=use_list)
+        assert (np.abs(PA.f64(P.out[s]) - want) <= PA.attention_bound(want, "bf16")).all()
+        assert np.abs(PA.f64(P.lse[s]) - lse).max() <= 1e-3
