@@ -179,7 +179,8 @@ def make_params(q, k_cache, out, ctx_len, *, n_retain, kv_budget=0, budget_frac=
 
 def make_mx_cache(kv_format, k_scale, v_scale) -> QuokaMxCache:
     """Describe a microscaled cache: k_scale, v_scale are uint8 tensors of the cache's shape with d / 32 scale bytes
-    in the place of a row's elements, dense (contiguous (b, n_KV, rows, d / 32) or (pages, n_KV, 64, d / 32))."""
+    in the place of a row's elements, dense (contiguous (b, n_KV, rows, d / 32) or (pages, n_KV, 64, d / 32)).  Addresses only:
+    the caller keeps the tensors."""
     if not (k_scale.is_contiguous() and v_scale.is_contiguous()):
         raise ValueError("the scale tensors of a microscaled cache are dense")
     return QuokaMxCache(int(kv_format), k_scale.data_ptr(), v_scale.data_ptr())

@@ -5,7 +5,7 @@
 //   the conversion instruction.  The inverse norm of a key row is that of the values the cache then holds.
 // read: cache rows first .. first + n - 1 to dense [b][n_KV][n][D] tensors; rows at and beyond T_s + C are left as they were.
 //   A lane turns 8 elements of K and of V into 16 (bf16) or 32 bytes (f32).
-// Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 101 us, 5.5 TB/s of 0.56 GB); a generation step's rows by the launch.
+// Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 91 us, 6.2 TB/s of 0.57 GB); a generation step's rows by the launch.
 #include "mx.cuh"
 #include "mx_host.cuh"
 
@@ -112,19 +112,15 @@ __device__ __forceinline__ void piece_values(uint2 w, float scale, float (&x)[8]
     x[i] = mx_element<FMT>(code) * scale;
   }
 }
-template <typename E>
-__device__ __forceinline__ void store8(E* p, const float (&x)[8]) {
+template <typename E, int FMT>
+__device__ __forceinline__ void store_values(E* p, const uint2& w, uint32_t scale) {
   if constexpr (sizeof(E) == 4) {
+    float x[8];
+    piece_values<FMT>(w, mx_scale(scale), x);
     reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(p) = mx_values_bf16x8<FMT>(w.x, w.y, mx_scale_bf16x2(scale));
   }
 }
 
@@ -156,19 +152,14 @@ __global__ void __launch_bounds__(kMxThreads) read_kv_mx_kernel(DevParams P, con
   for (int j = 0; j < UNR; ++j) {
     if (r0 + j * RPP >= rows) break;
     const int64_t to = ((int64_t)unit * n_rows + r0 + j * RPP) * D + c * 8;
-    float x[8];
-    piece_values<FMT>(kw[j], mx_scale(kb[j]), x);
-    store8(k_out + to, x);
-    if (v_cache) {
-      piece_values<FMT>(vw[j], mx_scale(vb[j]), x);
-      store8(v_out + to, x);
-    }
+    store_values<E, FMT>(k_out + to, kw[j], kb[j]);
+    if (v_cache) store_values<E, FMT>(v_out + to, vw[j], vb[j]);
   }
 }
 
 // ---------------------------------------------------------------------------------------------- host
-// Rows per thread: four where the CTAs then still make two waves, else one.  One / four, us, 8 KV heads, d 128, MXFP8: append of 8 times 4096 rows 41.0 / 36.7,
-// 16 of one row 7.2 / 7.4, read of 8192 rows 13.1 / 9.4, of 2000 rows 5.9 / 6.1, of 4 sequences of 20011 to 32768 rows 162 / 112 (MXFP4 161 / 101).
+// Rows per thread: four where the CTAs then still make two waves, else one.  One / four, us, 8 KV heads, d 128, MXFP8: append of 8 times 4096 rows 40.4 / 36.5,
+// 16 of one row 7.2 / 7.4, read of 8192 rows 12.6 / 7.8, of 2000 rows 5.9 / 6.1, of 4 sequences of 20011 to 32768 rows 162 / 104 (MXFP4 161 / 90).
 struct MxGrid { int unr, tiles; int64_t ctas; };
 static MxGrid mx_grid(const DevParams& P, int64_t rows) {
   const int64_t units = (int64_t)P.batch * P.n_kv;

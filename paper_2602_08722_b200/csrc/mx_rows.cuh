@@ -25,11 +25,6 @@ template <int FMT>
 __device__ __forceinline__ uint32_t mx_factor2(uint32_t b) { return ((b + (FMT == QUOKA_KV_MXFP8 ? 120u - kMxShift : 126u - kMxShift)) << 7) * 0x10001u; }
 constexpr uint32_t kBf16Nan2 = 0x7FC07FC0u;
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  uint32_t d;
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
 // The 8 elements of half a unit (two words of MXFP8, one of MXFP4) as four bf16 pairs, in the order in which their bits are reached by
 // shifts and masks alone: 0 2 1 3 4 6 5 7, or 0 4 1 5 2 6 3 7 (mx_place).  Queries are put in the same order once per CTA, so that products
 // are the same; the columns of O come out in it, and the epilogues take them from there.  Against the plain order, by byte
@@ -55,19 +50,9 @@ template <int FMT, bool PLAIN = false>
 __device__ __forceinline__ uint4 mx_to_bf16x8(uint32_t w0, uint32_t w1, uint32_t factor2) {
   uint32_t o[4];
   if constexpr (PLAIN) {
-    if constexpr (FMT == QUOKA_KV_MXFP8) {
-      o[0] = __byte_perm(w0, w0, 0x1100); o[1] = __byte_perm(w0, w0, 0x3322);
-      o[2] = __byte_perm(w1, w1, 0x1100); o[3] = __byte_perm(w1, w1, 0x3322);
-    } else {
-      const uint32_t lo = w0 << 4;
-      o[0] = __byte_perm(lo, w0, 0x4400); o[1] = __byte_perm(lo, w0, 0x5511);
-      o[2] = __byte_perm(lo, w0, 0x6622); o[3] = __byte_perm(lo, w0, 0x7733);
-    }
+    mx_bits_bf16x8<FMT>(w0, w1, o);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {                      // (what stands below an element's bits is masked off)
-      o[i] = (o[i] & 0x80008000u) | (FMT == QUOKA_KV_MXFP8 ? o[i] >> 4 & 0x07F007F0u : o[i] >> 6 & 0x01C001C0u);
-      o[i] = mul_bf16x2(o[i], factor2);
-    }
+    for (int i = 0; i < 4; ++i) o[i] = mul_bf16x2(o[i], factor2);
   } else if constexpr (FMT == QUOKA_KV_MXFP8) {
     uint32_t a[2], b[2];
     mx_to_pairs<FMT>(w0, factor2, a);

@@ -11,7 +11,7 @@
 // cached rows, takes 917 us against 858 us over a bf16 cache.
 //
 // The rule (kUnpackFrom), query rows per KV head; both ways, us, converted in the loaders / unpacked first, MXFP8:
-//   listed 3932 of 32768, d 128:  1024 rows 40.2 / 42.5, 2048 57.5 / 55.4, 4096 85.7 / 79.3, 8192 170 / 150
+//   listed 3932 of 32768, d 128:  1024 rows 40.2 / 42.5, 2048 57.5 / 55.4, 4096 85.7 / 79.3, 8192 170 / 147
 //   listed 3932 of 20011, d 64:   1024 rows 32.9 / 35.2, 2048 49.1 / 47.2, 3108 80.0 / 71.7
 //   all of 20011, d 64:           512 rows 57.4 / 61.6, 1024 82.0 / 81.8, 2048 148 / 137, 3108 233 / 214
 //   all of 32768, d 128:          1024 rows 148 / 170, 2048 243 / 262, 4096 490 / 491, 8192 969 / 917
@@ -68,30 +68,10 @@ __global__ void __launch_bounds__(kUnpackThreads) unpack_rows_mx_kernel(DevParam
     const int r = r0 + j * RPP;
     if (r >= rows) break;
     const int64_t to = ((int64_t)unit * pitch + r) * LPR + c;
-    const float f = mx_scale(kb[j]);
-    float x[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = mx_element<FMT>(FMT == QUOKA_KV_MXFP8 ? (i < 4 ? kw[j].x : kw[j].y) >> (8 * (i % 4)) & 0xFFu : kw[j].x >> (4 * i) & 0xFu) * f;
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    k_out[to] = make_uint4(w[0], w[1], w[2], w[3]);
+    k_out[to] = mx_values_bf16x8<FMT>(kw[j].x, kw[j].y, mx_scale_bf16x2(kb[j]));
     const bool bad = vb[j] == kMxNanScale;
     if (bad && c % 4 == 0) atomicMin(nan_pos + c / 4, max(r - cnt, -1));
-    const float fv = bad ? 0.f : mx_scale(vb[j]);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      x[i] = mx_element<FMT>(FMT == QUOKA_KV_MXFP8 ? (i < 4 ? vw[j].x : vw[j].y) >> (8 * (i % 4)) & 0xFFu : vw[j].x >> (4 * i) & 0xFu) * fv;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    v_out[to] = make_uint4(w[0], w[1], w[2], w[3]);
+    v_out[to] = mx_values_bf16x8<FMT>(vw[j].x, vw[j].y, bad ? 0u : mx_scale_bf16x2(vb[j]));
   }
   __syncthreads();
   if (threadIdx.x < BLOCKS) v_nan[(size_t)blockIdx.x * BLOCKS + threadIdx.x] = nan_pos[threadIdx.x];

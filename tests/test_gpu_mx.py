@@ -538,3 +538,29 @@ def test_few_rows_shared_in_clusters(use_list, fmt, n_q, n_kv, d, lens, C, paged
         want, lse = P.reference(s, use_list=use_list)
         assert (np.abs(PA.f64(P.out[s]) - want) <= PA.attention_bound(want, "bf16")).all()
         assert np.abs(PA.f64(P.lse[s]) - lse).max() <= 1e-3
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_code_under_every_scale_reads_back(fmt, d, dtype):
+    """quoka_read_kv_mx of scales that this library does not write too: the value, rounded once where bf16 or fp32 ends."""
+    codes = 256 if fmt == api.KV_MXFP8 else 16
+    code = (np.arange(256)[:, None] * 7 + np.arange(d * 8)).reshape(1, 1, 256 * 8, d) % codes
+    code[np.isin(code, (0x7F, 0xFF)) & (fmt == api.KV_MXFP8)] = 0
+    scale = np.repeat(np.arange(256), 8 * d // 32).reshape(1, 1, 2048, d // 32)
+    kc, vc = (torch.from_numpy(R.pack(code.astype(np.uint8), fmt)).cuda() for _ in range(2))
+    ks, vs = (torch.from_numpy(scale.astype(np.uint8)).cuda() for _ in range(2))
+    q = torch.zeros(1, 1, 1, d, dtype=DTYPES[dtype], device="cuda")
+    ctx = torch.tensor([2047], dtype=torch.int32, device="cuda")
+    p = api.make_params(q, kc, torch.empty_like(q), ctx, n_retain=1, kv_budget=1, max_ctx_len=2047, kv_format=fmt)
+    mx = api.make_mx_cache(fmt, ks, vs)
+    k, v = (torch.zeros(1, 1, 2048, d, dtype=DTYPES[dtype], device="cuda") for _ in range(2))
+    api.quoka_read_kv_mx(p, mx, kc, vc, 0, 2048, k, v, api.alloc_workspace(p, mx=mx))
+    unit = R.values(code.astype(np.uint8), np.full_like(scale, 127).astype(np.uint8), fmt)
+    with np.errstate(invalid="ignore", over="ignore"):
+        want = unit * np.where(np.repeat(scale, 32, axis=-1) == 255, np.nan, np.exp2(np.repeat(scale, 32, axis=-1) - 127.0))
+        want = torch.from_numpy(want).to(torch.float32).to(DTYPES[dtype])
+    for got in (k.cpu(), v.cpu()):
+        assert torch.equal(torch.isnan(got), torch.isnan(want))
+        assert torch.equal(got[~torch.isnan(want)], want[~torch.isnan(want)])
