@@ -564,3 +564,66 @@ def test_every_code_under_every_scale_reads_back(fmt, d, dtype):
     for got in (k.cpu(), v.cpu()):
         assert torch.equal(torch.isnan(got), torch.isnan(want))
         assert torch.equal(got[~torch.isnan(want)], want[~torch.isnan(want)])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n_q,n_kv,d,C", [(8, 2, 128, 1), (8, 1, 64, 5), (8, 1, 64, 260), (8, 2, 128, 70)])
+def test_a_captured_call_follows_the_lengths_on_the_device(fmt, n_q, n_kv, d, C):
+    inp = synth.make_chunk_inputs(23, 2, n_q, n_kv, d, [2500, 2500], C, "bf16")
+    P = R.MxProblem(inp, fmt, n_retain=4, kv_budget=300)
+    dense = torch.empty_like(P.out)
+
+    def calls(stream=None):
+        api.quoka_prefill_chunk_mx(P.p, P.mx, P.q, P.k, P.v, P.out, None, None, P.ws, stream=stream)
+        api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, dense, None, P.ws, stream=stream)
+    calls()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        calls(side)
+    for lens in ([2500, 2500], [1, 2500], [0, 31], [777, 300], [299, 0]):
+        P.ctx_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = P.out.clone(), dense.clone()
+        P.out.zero_(), dense.zero_()
+        calls()
+        torch.cuda.synchronize()
+        assert torch.equal(got[0], P.out) and torch.equal(got[1], dense)
+        assert torch.isfinite(got[0].float()).all() and torch.isfinite(got[1].float()).all()
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_two_streams_at_once(fmt):
+    """Calls on two streams with a workspace each: few rows in clusters beside a chunk whose rows are unpacked."""
+    problems = [R.MxProblem(synth.make_chunk_inputs(51, 1, 8, 2, 128, [3000], 1, "bf16"), fmt, n_retain=1, kv_budget=1500),
+                R.MxProblem(synth.make_chunk_inputs(52, 2, 8, 1, 64, [1000, 77], 300, "bf16"), fmt, n_retain=8, kv_budget=200, paged=True)]
+
+    def call(P, out, stream=None):
+        api.quoka_prefill_chunk_mx(P.p, P.mx, P.q, P.k, P.v, out, None, None, P.ws, stream=stream)
+    want = []
+    for P in problems:
+        call(P, P.out)
+        want.append(P.out.clone())
+    streams = [torch.cuda.Stream() for _ in problems]
+    torch.cuda.synchronize()
+    for _ in range(30):
+        for P, s in zip(problems, streams):
+            call(P, P.out, s)
+    torch.cuda.synchronize()
+    for P, w in zip(problems, want):
+        assert torch.equal(P.out, w) and api.quoka_last_device_status(P.ws) == 0
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("n_q,n_kv,d,C", [(8, 2, 128, 1), (8, 1, 64, 4), (8, 2, 128, 70), (8, 1, 64, 260), (8, 1, 128, 300)])
+def test_lists_that_are_empty_short_or_name_a_row_twice(fmt, n_q, n_kv, d, C):
+    inp = synth.make_chunk_inputs(27, 3, n_q, n_kv, d, [900, 900, 40], C, "bf16")
+    P = R.MxProblem(inp, fmt, kv_budget=850)
+    P.listed(9, counts=[0, 801, 40])
+    P.idx_host[1, :, 5] = P.idx_host[1, :, 4]
+    P.idx_host[1, :, :7] = P.idx_host[1, :, :7][:, ::-1]               # (nor in order)
+    k_idx, k_cnt = torch.from_numpy(P.idx_host).cuda(), torch.tensor(P.cnt_host, dtype=torch.int32, device="cuda")
+    api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, P.out, None, P.ws)
+    torch.cuda.synchronize()
+    for s in range(3):
+        PA.check_attention(PA.f64(P.out[s]), P.reference(s, use_list=True)[0], "bf16")
