@@ -6,6 +6,8 @@
 // read: cache rows first .. first + n - 1 to dense [b][n_KV][n][D] tensors; rows at and beyond T_s + C are left as they were.
 //   A lane turns 8 elements of K and of V into 16 (bf16) or 32 bytes (f32).
 // Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 91 us, 6.2 TB/s of 0.57 GB); a generation step's rows by the launch.
+#include <cuda_fp16.h>
+
 #include "mx.cuh"
 #include "mx_host.cuh"
 
@@ -13,37 +15,84 @@ namespace quoka {
 
 constexpr int kMxThreads = 256;
 
-// 8 new elements as floats.
-template <typename E>
-__device__ __forceinline__ void load8(const E* p, float (&x)[8]) { load_vec<E, 8, true>(p, x); }
-
-// This lane's 8 elements to codes in w (MXFP8: two words, MXFP4: one) with their block's scale byte; x becomes the values the cache holds.
-template <int FMT>
-__device__ __forceinline__ uint32_t mx_quantise8(float (&x)[8], uint32_t (&w)[2]) {
-  uint32_t amax = 0;                                 // (bits of magnitudes order like the magnitudes, NaN above infinity)
+// 8 new elements: floats, or bf16 pairs, which stay pairs as long as they can (append of 8 times 4096 rows, 8 heads, d 128: 34.7 us, as floats
+// 36.5, MXFP4 36.7 / 39.8).
+template <typename E> struct MxNew;
+template <> struct MxNew<float> {
+  float x[8];
+  __device__ __forceinline__ void load(const float* p) { load_vec<float, 8, true>(p, x); }
+  // bits of the largest magnitude (they order like the magnitudes, NaN above infinity)
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) amax = max(amax, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(x[i]) & 0x7FFFFFFFu);
+    return m;
+  }
+  // a pair times 2^-e: exact
+  __device__ __forceinline__ float2 pair(int i, int e) const {
+    const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+    return make_float2(x[2 * i] * down, x[2 * i + 1] * down);
+  }
+};
+template <> struct MxNew<__nv_bfloat16> {
+  uint4 w;
+  __device__ __forceinline__ void load(const __nv_bfloat16* p) { w = load_input<true>(reinterpret_cast<const uint4*>(p)); }
+  __device__ __forceinline__ uint32_t word(int i) const { return i == 0 ? w.x : i == 1 ? w.y : i == 2 ? w.z : w.w; }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) m = __vmaxu2(m, word(i) & 0x7FFF7FFFu);
+    return max(m & 0xFFFF0000u, m << 16);
+  }
+  // exact but for what becomes zero whatever is left of it
+  __device__ __forceinline__ float2 pair(int i, int e) const {
+    const uint32_t y = mul_bf16x2(word(i), ((uint32_t)(127 - e) << 7) * 0x10001u);
+    return make_float2(__uint_as_float(y << 16), __uint_as_float(y & 0xFFFF0000u));
+  }
+};
+
+// A pair of elements as numbers.
+template <int FMT>
+__device__ __forceinline__ float2 mx_decode2(uint32_t c) {
+  uint32_t h;
+  if constexpr (FMT == QUOKA_KV_MXFP8) asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"((uint16_t)c));
+  else asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h) : "r"(c));
+  return __half22float2(*reinterpret_cast<const __half2*>(&h));
+}
+
+// This lane's 8 elements to codes in w (MXFP8: two words, MXFP4: one) with their block's scale byte; `square`: the sum of the squares of the values
+// the cache then holds (NaN where it holds NaN), where it is asked for.
+template <int FMT, typename E>
+__device__ __forceinline__ uint32_t mx_quantise8(const MxNew<E>& x, uint32_t (&w)[2], bool want_square, float& square) {
+  uint32_t amax = x.largest();
   amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 1));
   amax = max(amax, __shfl_xor_sync(0xFFFFFFFFu, amax, 2));
   const bool finite = amax < 0x7F800000u;
   const int e = mx_scale_exponent<FMT>(amax);
-  const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23);
   uint32_t c[4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i)                        // (the product is exact: a value times a power of two)
-    c[i] = finite ? mx_encode2<FMT>(x[2 * i] * down, x[2 * i + 1] * down) : 0u;
+  for (int i = 0; i < 4; ++i) {
+    const float2 y = x.pair(i, e);
+    c[i] = finite ? mx_encode2<FMT>(y.x, y.y) : 0u;
+  }
   if constexpr (FMT == QUOKA_KV_MXFP8) {
     w[0] = c[0] | c[1] << 16;
     w[1] = c[2] | c[3] << 16;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = mx_element<FMT>(w[i / 4] >> (8 * (i % 4)) & 0xFFu) * up;
   } else {
     w[0] = c[0] | c[1] << 8 | c[2] << 16 | c[3] << 24;
     w[1] = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = mx_element<FMT>(w[0] >> (4 * i) & 0xFu) * up;
   }
-  if (!finite) x[0] = __uint_as_float(0x7FC00000u);
+  if (want_square) {                                 // (squares of elements are exact in fp32, and so is their product with 2^(2 e) above 2^-126)
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float2 v = mx_decode2<FMT>(c[i]);
+      sum = fmaf(v.x, v.x, sum);
+      sum = fmaf(v.y, v.y, sum);
+    }
+    const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+    square = finite ? sum * up * up : __uint_as_float(0x7FC00000u);
+  }
   return finite ? (uint32_t)(e + 127) : kMxNanScale;
 }
 
@@ -66,22 +115,20 @@ __global__ void __launch_bounds__(kMxThreads) append_kv_mx_kernel(DevParams P, c
   const int h = unit % P.n_kv, s = unit / P.n_kv;
   const int64_t first = (int64_t)unit * P.chunk;
   const int T = load_input<true>(P.ctx_len + s);
-  float kx[UNR][8], vx[UNR][8];
+  MxNew<E> kx[UNR], vx[UNR];
 #pragma unroll
   for (int j = 0; j < UNR; ++j) {                     // (a row past the chunk reads the last one; it is not written)
     const int64_t row = first + min(r0 + j * RPP, P.chunk - 1);
-    load8(k_new + row * D + c * 8, kx[j]);
-    load8(v_new + row * D + c * 8, vx[j]);
+    kx[j].load(k_new + row * D + c * 8);
+    vx[j].load(v_new + row * D + c * 8);
   }
 #pragma unroll
   for (int j = 0; j < UNR; ++j) {
     const int r = r0 + j * RPP, t = T + r;
     uint32_t kw[2], vw[2];
-    const uint32_t kb = mx_quantise8<FMT>(kx[j], kw), vb = mx_quantise8<FMT>(vx[j], vw);
-    float nn = 0.f;
+    float nn = 0.f, unused;
+    const uint32_t kb = mx_quantise8<FMT>(kx[j], kw, k_inv_norm != nullptr, nn), vb = mx_quantise8<FMT>(vx[j], vw, false, unused);
     if (k_inv_norm != nullptr) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) nn = fmaf(kx[j][i], kx[j][i], nn);
 #pragma unroll
       for (int o = LPR / 2; o > 0; o >>= 1) nn += __shfl_xor_sync(0xFFFFFFFFu, nn, o);
     }
@@ -158,7 +205,7 @@ __global__ void __launch_bounds__(kMxThreads) read_kv_mx_kernel(DevParams P, con
 }
 
 // ---------------------------------------------------------------------------------------------- host
-// Rows per thread: four where the CTAs then still make two waves, else one.  One / four, us, 8 KV heads, d 128, MXFP8: append of 8 times 4096 rows 40.4 / 36.5,
+// Rows per thread: four where the CTAs then still make two waves, else one.  One / four, us, 8 KV heads, d 128, MXFP8: append of 8 times 4096 rows 39.3 / 34.7,
 // 16 of one row 7.2 / 7.4, read of 8192 rows 12.6 / 7.8, of 2000 rows 5.9 / 6.1, of 4 sequences of 20011 to 32768 rows 162 / 104 (MXFP4 161 / 90).
 struct MxGrid { int unr, tiles; int64_t ctas; };
 static MxGrid mx_grid(const DevParams& P, int64_t rows) {
