@@ -466,7 +466,7 @@ template <int D>
 __device__ __forceinline__ void attn_load_nan(const DevParams& P, int* v_nan, int s, int kv, int rows) {
   if (threadIdx.x < D / kMxBlock) v_nan[threadIdx.x] = kNoNan;
   __syncthreads();
-  const int tiles = (rows + P.v_nan_rows - 1) / P.v_nan_rows;
+  const int tiles = min((rows + P.v_nan_rows - 1) / P.v_nan_rows, P.v_nan_tiles);
   const int32_t* from = P.v_nan + ((size_t)s * P.n_kv + kv) * P.v_nan_tiles * (D / kMxBlock);
   for (int i = threadIdx.x; i < tiles * (D / kMxBlock); i += blockDim.x) {
     const int at = __ldcg(from + i);

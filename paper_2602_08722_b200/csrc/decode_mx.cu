@@ -687,13 +687,14 @@ static cudaError_t launch_decode_mx_t(const DevParams& P, const void* q, const v
   //   a cluster per unit   1000 rows on: 12.3 / 12.3 / 12.3 / 14.4 / 16.4 / 20.5 / 28.7 (of 10 CTAs: on a B200 seven clusters of 11 to 16 are resident, 11 of 10)
   //   one list             16.4 to 4003 rows / 20.5 / 22.9 / 28.7: joining parts costs a launch and a round trip through L2, some 3 rounds of the warps
   // so a CTA to 24 granules (four positions over 700 rows: 14.4 alone, 16.4 in clusters), then clusters where they take 3 rounds more than the list at
-  // most.  Sequences of a batch may differ, and their clusters do not help each other: 4 rounds at most.  (8 sequences of 1500 rows: 14.4, as a list 20.5.)
+  // most, which takes what its longest sequence needs or more: sequences of a batch may differ, and their clusters do not help each other.  (8
+  // sequences of 1500 rows: 14.4, as a list 20.5; two of 9393 rows 20.5 / 23.7, of 9393 and 100 20.5 / 22.6.)
   // No clusters: a CTA to 4 rounds (the same 8 sequences 16.4), or where units are many.
   int per_unit = most <= kDecWhole || units >= 64ll * sms ? 1 : 0;
   if (per_unit == 0) {
     const int cl = largest_cluster<FMT, D, NT>(units, smem);
     const auto rounds = [&](long long granules, long long over) { return (granules + over * WARPS - 1) / (over * WARPS); };
-    if (cl > 1 && rounds(most, cl) <= 3 + (P.batch == 1 ? rounds(units * most, sms) : 1)) per_unit = cl;
+    if (cl > 1 && rounds(most, cl) <= 3 + rounds(units / P.batch * most, sms)) per_unit = cl;
     else if (most <= 4 * WARPS) per_unit = 1;
   }
   const long long ctas = per_unit > 0 ? units * per_unit : std::min<long long>(sms, (units * most + WARPS - 1) / WARPS);
