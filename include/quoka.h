@@ -173,7 +173,8 @@ quoka_status quoka_select_keys(const quoka_params* p, const float* scores, int32
 
 /* Alg. 2, the attention line, with Eq. 1/Eq. 2 semantics: row r of query head h
  * attends rows k_idx[s][h/G][0..k_cnt[s]) of the ORIGINAL cache plus the chunk's
- * own rows T_s..T_s+r (causal, diagonal included); softmax in fp32.  The rows are
+ * own rows T_s..T_s+r (causal, diagonal included); softmax in fp32.  The list may name any
+ * rows < T_s in any order, a row named twice counts twice.  The rows are
  * gathered inside the kernel; no compacted copy of K or V is made.
  *   out [b][n_Q][C][d] by strides, `dtype`;  lse [b][n_Q][C] fp32 natural-log-sum-exp of
  *   the scaled logits, may be NULL */

@@ -279,7 +279,8 @@ DevParams attn_of_plan(const DevParams& P0, const AttnPlan& plan) {
 quoka_status launch_attn_tc(const quoka_params* p, const DevParams& P0, const void* q, const void* k, const void* v,
                             const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st,
                             bool after_selection, const AttnPlan& plan) {
-  const DevParams P = attn_of_plan(P0, plan);
+  DevParams P = attn_of_plan(P0, plan);
+  P.list_of_selection = after_selection ? 1 : 0;
   if (plan.ctas == 2) return launch_attn_tc_pair(p, P, q, k, v, k_idx, k_cnt, out, lse, st, after_selection, plan);
   CUtensorMap tm_q, tm_k, tm_v;
   if (!encode_q_tensor_map(&tm_q, P, q)) return QUOKA_ERR_CUDA;

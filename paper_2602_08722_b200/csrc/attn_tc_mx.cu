@@ -24,7 +24,8 @@ static AttnKernel pick(bool sparse, bool parts, bool in_cluster) {
 quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P0, int fmt, const void* q, const void* k, const void* v,
                                const int32_t* k_idx, const int32_t* k_cnt, void* out, float* lse, cudaStream_t st, bool after_selection,
                                const AttnPlan& plan) {
-  const DevParams P = attn_of_plan(P0, plan);
+  DevParams P = attn_of_plan(P0, plan);
+  P.list_of_selection = after_selection ? 1 : 0;
   CUtensorMap tm_q, tm_k, tm_v;
   if (!encode_q_tensor_map(&tm_q, P, q)) return QUOKA_ERR_CUDA;
   // (a pair's CTA takes half of V's columns)

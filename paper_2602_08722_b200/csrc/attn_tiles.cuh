@@ -116,6 +116,7 @@ struct AttnGeom {
   bool active_b;      // must live in registers (an indexed member would put it in local memory)
   int n_known;        // tiles known so far (sparse: n_chunk until resolved, then n_chunk + n_sel)
   int cnt;            // sparse: selected rows (valid once resolved)
+  int in_order;       // sparse: a list of this many rows is the cache's rows in order (-1: a caller's list may be any rows)
   int n_dense;        // dense: number of tiles
   bool resolved;
 };
@@ -137,11 +138,12 @@ __device__ __forceinline__ AttnGeom make_geom(const DevParams& P, int s, int p, 
     g.skip_a = g.active_b ? g.n_chunk - (last_a / kKeyTile + 1) : 0;       // 0 or 1, for a pair up to 2: a Q tile spans at most 128 positions
     g.n_known = g.n_chunk;
     g.n_dense = 0;
+    g.in_order = P.list_of_selection ? g.T : -1;
     g.resolved = false;
   } else {
     g.n_dense = (g.T + last) / kKeyTile + 1;
     g.skip_a = g.active_b ? g.n_dense - ((g.T + last_a) / kKeyTile + 1) : 0;
-    g.n_chunk = 0; g.lead = 0;
+    g.n_chunk = 0; g.lead = 0; g.in_order = -1;
     g.n_known = g.n_dense;
     g.resolved = true;
   }
@@ -196,9 +198,9 @@ __device__ __forceinline__ TileRows tile_rows(const AttnGeom& g, int t) {
       r.count = g.C - ct * kKeyTile;
       r.col0 = ct * kKeyTile;
     } else {
-      // a list as long as the cache is the identity (the budget covers the cache): its tiles are plain row ranges
+      // the selection's list is the rows in order where the budget covers the cache: its tiles are plain row ranges
       const int st = t - g.n_chunk;
-      r.from_list = g.cnt != g.T;
+      r.from_list = g.cnt != g.in_order;
       r.causal = false;
       r.first = st * kKeyTile;
       r.count = g.cnt - st * kKeyTile;

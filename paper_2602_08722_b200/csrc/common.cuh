@@ -51,6 +51,7 @@ struct DevParams {
   int attn_row_blocks, attn_split_rb, attn_parts, attn_after_whole;
   int attn_pack, attn_span;   // heads and chunk positions of a Q tile of 128 rows
   int attn_qtiles;            // Q tiles of a CTA, 1 or 2
+  int list_of_selection;      // tensor-core attention: the list was made by the key selection, ascending and each row once
 };
 
 // B_s of one sequence: min(B_SA, T) or floor(frac*T + 0.5) in double.

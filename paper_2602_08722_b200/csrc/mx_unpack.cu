@@ -41,7 +41,7 @@ __global__ void __launch_bounds__(kUnpackThreads) unpack_rows_mx_kernel(DevParam
   if (tile * kUnpackTile<D> >= rows) return;
   if (threadIdx.x < BLOCKS) nan_pos[threadIdx.x] = kNoNan;
   __syncthreads();
-  const int32_t* idx = k_idx && cnt != T ? k_idx + (int64_t)unit * P.budget_cap : nullptr;
+  const int32_t* idx = k_idx && !(P.list_of_selection && cnt == T) ? k_idx + (int64_t)unit * P.budget_cap : nullptr;
   int t[UNR];
 #pragma unroll
   for (int j = 0; j < UNR; ++j) {                     // (a row past the end reads the last one; it is not written)
@@ -101,24 +101,25 @@ size_t attn_unpack_bytes(const quoka_params* p, bool listed) {
 static AttnKernel pick_unpacked_pair(bool sparse, bool parts, bool in_cluster) { return pick_attn_tc_pair<kUnpacked>(sparse, parts, in_cluster); }
 
 quoka_status launch_attn_mx_unpacked(const quoka_params* p, const DevParams& P0, int fmt, const void* q, const void* k, const void* v, const int32_t* k_idx,
-                                     const int32_t* k_cnt, void* out, float* lse, void* scratch, cudaStream_t st, bool chained, const AttnPlan& plan) {
+                                     const int32_t* k_cnt, void* out, float* lse, void* scratch, cudaStream_t st, bool after_selection, const AttnPlan& plan) {
   const bool listed = k_idx != nullptr;
   const int rows = (int)unpack_rows(p, listed);
   unsigned char* base = static_cast<unsigned char*>(scratch);
   void *ku = base, *vu = base + unpack_side(p, listed);
   int32_t* v_nan = reinterpret_cast<int32_t*>(base + 2 * unpack_side(p, listed));
   DevParams P = attn_of_plan(P0, plan);
+  P.list_of_selection = after_selection ? 1 : 0;
   P.v_nan = v_nan;
   P.v_nan_rows = unpack_tile(p);
   P.v_nan_tiles = (int)unpack_tiles(p, listed);
   const unsigned ctas = (unsigned)((long long)P.batch * P.n_kv * P.v_nan_tiles);
   const cudaError_t e = mx_dispatch(QUOKA_BF16, fmt, P.d, [&](auto, auto f, auto d) {
-    return launch_kernel("unpack_rows_mx", unpack_rows_mx_kernel<f.value, d.value>, dim3(ctas), dim3(kUnpackThreads), 0, st, 1, chained, P, (const uint8_t*)k,
+    return launch_kernel("unpack_rows_mx", unpack_rows_mx_kernel<f.value, d.value>, dim3(ctas), dim3(kUnpackThreads), 0, st, 1, after_selection, P, (const uint8_t*)k,
                          (const uint8_t*)v, k_idx, k_cnt, rows, (uint4*)ku, (uint4*)vu, v_nan);
   });
   if (e != cudaSuccess) return QUOKA_ERR_CUDA;
   count_launch();
-  // From here on a bf16 cache of `rows` rows: a list as long as the cache is the identity.
+  // From here on a bf16 cache of `rows` rows, k_cnt of them listed: all, in order.
   quoka_params pu = *p;
   pu.page_size = 0; pu.max_pages_per_seq = 0; pu.block_table = nullptr;
   pu.kv_rows = rows;
@@ -126,7 +127,7 @@ quoka_status launch_attn_mx_unpacked(const quoka_params* p, const DevParams& P0,
   P.page_size = 0; P.max_pages = 0; P.block_table = nullptr;
   P.kv_rows = rows;
   P.kv_st = pu.kv_stride_t; P.kv_sh = pu.kv_stride_h; P.kv_sb = pu.kv_stride_b;
-  if (listed) P.ctx_len = k_cnt;
+  if (listed) { P.ctx_len = k_cnt; P.list_of_selection = 1; }
   CUtensorMap tm_q, tm_k, tm_v;
   if (!encode_q_tensor_map(&tm_q, P, q) || !encode_kv_tensor_map(&tm_k, &pu, ku, 64) || !encode_kv_tensor_map(&tm_v, &pu, vu, 64)) return QUOKA_ERR_CUDA;
   const bool pair = plan.ctas == 2, wide = P.d == 128;

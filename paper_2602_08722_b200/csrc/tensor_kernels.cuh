@@ -56,6 +56,6 @@ quoka_status launch_attn_mx_tc(const quoka_params* p, const DevParams& P, int fm
 // Long chunks: rows unpacked into scratch first (mx_unpack.cu); attn_unpack_bytes: what that takes, 0 where it is not done
 size_t attn_unpack_bytes(const quoka_params* p, bool listed);
 quoka_status launch_attn_mx_unpacked(const quoka_params* p, const DevParams& P, int fmt, const void* q, const void* k, const void* v, const int32_t* k_idx,
-                                     const int32_t* k_cnt, void* out, float* lse, void* scratch, cudaStream_t st, bool chained, const AttnPlan& plan);
+                                     const int32_t* k_cnt, void* out, float* lse, void* scratch, cudaStream_t st, bool after_selection, const AttnPlan& plan);
 
 }  // namespace quoka
