@@ -265,7 +265,9 @@ quoka_status quoka_prefill_chunk_static(const quoka_params* p, const void* q, co
  * (impl = QUOKA_IMPL_SIMT) only; elsewhere their values are undefined.
  *
  * Every value of such a cache is a bf16 number exactly: attention and scores are those of a bf16 cache that holds the values
- * quoka_read_kv_mx returns, with the same sums (bf16 softmax weights, fp32 accumulation).
+ * quoka_read_kv_mx returns.  Products are exact and added up in fp32.  Softmax weights are bf16; calls of a few query rows (see
+ * quoka_workspace_size_mx) have fp16 weights, of which those 2^-32 times a row's largest and less vanish, wherever the scales of the values
+ * in 32 columns are within 2^9 of each other.
  *
  * quoka_params describes the cache as ever, strides in ELEMENTS (two to a byte for MXFP4), multiples of 32.  dtype is the type of
  * q, qbar, out, of the rows appended and of those read back.  f32 queries take the scalar kernels.  The chunk's own rows

@@ -3,26 +3,31 @@
 //
 // What bounds it: HBM (every row of the cache is read once and used for a dozen multiplications), and next to it the instructions
 // that turn 8 or 4 bits into operands.  So the products are matrix instructions with the keys on the M side (m16n8k16: the query
-// rows fill the 8 columns, a 128-row tcgen05 tile would have 4 or 8 rows of use in 128), whose operands a lane builds in registers from the
-// bytes it copied itself:
-//   S^T = K Q^T   a lane brings 16-byte pieces of key rows; which columns they are does not matter to the sum, Q's fragment has the same
-//   O^T = V^T P^T a lane brings the same 8 or 16 columns of value rows and interleaves the rows of a pair
-// P^T comes out of S^T by 8 x 8 transpositions (movmatrix).  Nothing but the scale words crosses lanes on the way in.
+// rows fill the 8 columns, a 128-row tcgen05 tile would have 4 or 8 rows of use in 128), whose operands a lane builds in registers from raw
+// bytes:
+//   S^T = K Q^T   a lane reads 16-byte pieces of key rows; which columns they are does not matter to the sum, Q's fragment has the same
+//   O^T = V^T P^T a lane reads the same 8 or 16 columns of value rows and interleaves the rows of a pair
+// P^T comes out of S^T by 8 x 8 transpositions (movmatrix).  The rows come into a ring of shared memory that a warp has for itself: 32
+// consecutive ones by the copy engine, of which lane 0 asks for a box and every lane waits on the barrier; others by cp.async of all lanes, each
+// waiting for its own and then for the warp.
 //
 // The operands are fp16, which the conversion instructions make of 8 and 4 bits at once (by shifts and masks, as bf16, it took twice
-// the instructions: 637 for 16 keys of 128 columns, 171 us for a step of 16 sequences of 8K to 32K rows).  Its range does not limit:
-//   K  each row is scaled by its largest block's exponent, which goes into the row's score in fp32;
-//   Q  each row by a power of two to 2^14 .. 2^15, taken off the score in fp32 (bf16 has 8 bits: nothing is lost but what is 2^-39 of the
-//      row's largest element);
-//   V  by the largest exponent a lane has met in its columns, to which O is rescaled if one 2^7 times that comes (rare);
-//   P  weights 2^(x - m), m a reference point that the largest exponent x exceeds by 7 when it is set and by 15 at most: weights below 2^-25, against a largest one of
-//      2^7 or more, vanish (a hundred thousand of them are 2^-15 of the sum).
+// the instructions: 637 for 16 keys of 128 columns, 171 us for a step of 16 sequences of 8K to 32K rows):
+//   K  each row is divided by its largest block's scale, which goes into the row's score in fp32;
+//   Q  each row is multiplied by a power of two to 2^14 .. 2^15, taken off the score in fp32;
+//   V  blocks are divided by a scale of O's columns, which follows the largest one met;
+//   P  weights 2^(x - m), m a reference point that the largest exponent x exceeds by 7 when it is set and by 15 at most.
+// Products are exact as long as fp16 holds the operands: blocks of a key 2^15 (4-bit elements 2^23) below its largest, elements of a query
+// 2^31 below its largest, blocks of values 2^9 below the largest of their columns.  Where a granule of 32 keys has others, and only there, its
+// scores or its weighted values are taken from bf16 operands, which hold every value of a cache: so what a key of no weight, or one that a row
+// does not see, is worth has no part in the row's rounding.  Weights are fp16 otherwise; those 2^-32 times the largest and less then vanish, against
+// values 2^9 times the others' at most.  To look for such granules takes 2 % of the time (135.7 us where the kernel without took 132.4, sixteen long sequences).
 //
 // Split: units are (sequence, KV head, row group).  Few keys: a CTA per unit, or a cluster of CTAs with an equal share of the unit's granules of
 // 32 keys each, whose results are added up through distributed shared memory.  Else the granules of all units are one list, cut into equal contiguous
 // shares, one per CTA, and a second kernel adds up the units that several CTAs share: long lists are balanced whatever the sequences' lengths
 // are.  Inside a CTA the warps take granules in turn, each with a running maximum, sum and output of its own, added up at the end of a unit's part.
-// All parts are added up in order.  Weights are rounded to fp16 for the product and divided by their sum as rounded, so that they add up to
+// All parts are added up in order.  Weights are rounded to fp16 (bf16) for the product and divided by their sum as rounded, so that they add up to
 // one; the log-sum-exp is that of the weights before.
 //
 // Measured, MXFP8 / MXFP4, us: 16 sequences of 8192 to 32768 rows, 8 KV heads of 4, d 128, one position: 132 / 128 (735 MB of MXFP8: 5.6 TB/s;
@@ -176,29 +181,32 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
   float o[NT][TILES][4], m[NT][2], l[NT][2], lx[NT][2];    // lx: the sum of the weights before they are rounded
   int stage = 0, s_cur = -1, kv_cur = -1, grp_cur = -1;
   uint32_t phase = 0;
+  bool wide_q = false;                                // a query row has elements that fp16 does not hold beside its largest one
   for (bool again = true; again;) {
     const int first_row = part.grp * ROWS, n_rows = min(ROWS, P.chunk * P.group - first_row);
     // ---- the part's query rows
     if (part.s != s_cur || part.kv != kv_cur || part.grp != grp_cur) {
       s_cur = part.s; kv_cur = part.kv; grp_cur = part.grp;
+      bool below = false;
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         const int row = 8 * nt + g, r = first_row + row;
         const __nv_bfloat16* qr = q + (long long)part.s * P.q_sb + (long long)(part.kv * P.group + r % P.group) * P.q_sh + (long long)(r / P.group) * P.q_st;
         uint4 w[D / 32];
-        uint32_t top = 0;                             // bits of the row's largest magnitude
+        DecMagnitudes mags;
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {             // 8 columns of the lane's D / 4
-          const int col = FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j;
           w[j] = make_uint4(0, 0, 0, 0);
-          if (row < n_rows) w[j] = load_input<true>(reinterpret_cast<const uint4*>(qr + col));
+          if (row < n_rows) w[j] = load_input<true>(reinterpret_cast<const uint4*>(qr + dec_column<FMT, D>(c, j)));
           const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = max(top, max(x[i] << 16 & 0x7FFF0000u, x[i] & 0x7FFF0000u));
+          for (int i = 0; i < 4; ++i) mags.take(x[i]);
         }
+        uint32_t top = mags.largest();
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         const int up = min(14 + 127 - (int)(top >> 23), 120);          // (an element that is not finite stays so)
+        below |= mags.below_f16(up);
         const float f = __uint_as_float((uint32_t)(127 + up) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
         for (int j = 0; j < D / 32; ++j) {
@@ -209,6 +217,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
         for (int e = 0; e < 2; ++e) qs[nt][e] = __shfl_sync(0xFFFFFFFFu, back, 4 * (2 * c + e)) * (P.scale * 1.4426950408889634f);
       }
+      wide_q = __any_sync(0xFFFFFFFFu, below);
     }
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
@@ -219,7 +228,12 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[nt][t][e] = 0.f;
     }
-    int ov = 0;                                        // scale byte of O's columns in this lane (all of one block of 32)
+    // Scale bytes of this lane's columns (all of one block of 32): O's; one less than the smallest of a block of values so far, and the
+    // largest that neither minds, in both halves of a word; whether blocks of values have differed too much for fp16 (in some lane).
+    int ov = 0;
+    uint32_t least = 0xFFFFFFFFu, passed = 0u;
+    bool wide_v = false;
+    const int v_shift = 8 * (D == 128 ? g >> 1 : g >> 2);
     int nan_u = kNoNan;                                // first key, in the order of visibility, with a value that is not finite in this lane's columns
     // keys that the rows of this lane's columns see: 2 c and 2 c + 1 of each tile
     int sees[NT][2];
@@ -245,14 +259,27 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
         }
         return w;
       };
+      // ---- scale bytes of the lane's eight values in its block of columns, two to a word
+      uint32_t ve[4], ve_most = passed, ve_low = least;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t e0 = scale_word(128, 2 * c + 8 * i) >> v_shift & 0xFFu, e1 = scale_word(128, 2 * c + 1 + 8 * i) >> v_shift & 0xFFu;
+        ve[i] = e0 | e1 << 16;
+        ve_most = __vmaxu2(ve_most, ve[i]);
+        ve_low = __viaddmin_u16x2(ve[i], 0xFFFFFFFFu, ve_low);         // (one less: a row that is not there has 0, and does not count)
+      }
+      const bool values_met = ve_most == passed && ve_low == least;
       // ---- S^T = K Q^T, 16 keys at a time
       float sc[2][NT][4];
+      DecFactors factors;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+      for (int h = 0; h < 2; ++h)
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
           for (int e = 0; e < 4; ++e) sc[h][nt][e] = 0.f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
         uint32_t w[2][KW], f[2][B::kKPieces];
         float key[2];
 #pragma unroll
@@ -270,6 +297,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
           for (int p = 0; p < B::kKPieces; ++p) {
             const float x = pow2_at_most_15((int)(sw >> (8 * (blk + 2 * p)) & 0xFFu) - (int)top);
             f[i][p] = f16x2(x, x);
+            factors.take(f[i][p]);
           }
         }
 #pragma unroll
@@ -291,25 +319,95 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       }
       // ---- softmax: a lane has keys g, g + 8, g + 16, g + 24 of rows 2 c and 2 c + 1; logits in log2 units
       const int u0 = gr * kDecGranule;
-      if (u0 + kDecGranule > all_see) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (u0 + 16 * h + g + 8 * (e >> 1) >= sees[nt][e & 1]) sc[h][nt][e] = -INFINITY;
-      }
       float top[NT][2];
-      bool grow = false;
+      const auto see = [&]() {                          // masks, maxima; whether the reference point of the exponentials is set, or moves
+        if (u0 + kDecGranule > all_see) {
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
+          for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          top[nt][e] = fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2]));
-          grow |= top[nt][e] > m[nt][e] + (float)kDecMaxAbove;
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                if (u0 + 16 * h + g + 8 * (e >> 1) >= sees[nt][e & 1]) sc[h][nt][e] = -INFINITY;
         }
-      if (__any_sync(0xFFFFFFFFu, grow)) {              // the reference point of the exponentials is set, or moves
+        bool grow = false;
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            top[nt][e] = fmaxf(fmaxf(sc[0][nt][e], sc[0][nt][e + 2]), fmaxf(sc[1][nt][e], sc[1][nt][e + 2]));
+            grow |= top[nt][e] > m[nt][e] + (float)kDecMaxAbove;
+          }
+        return grow;
+      };
+      // ---- do fp16 operands hold the granule, and the reference point: one vote, rarely with something to do
+      const bool keys_below = factors.below_f16<FMT>() || wide_q;
+      bool grow = see();
+      if (__any_sync(0xFFFFFFFFu, grow || keys_below || !values_met)) {
+        if (__any_sync(0xFFFFFFFFu, !values_met)) {
+          int most = 0, low = (int)(ve_low & 0xFFFFu) + 1;
+          low = min(low, (int)(ve_low >> 16) + 1);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t e = ve[i / 2] >> (16 * (i & 1)) & 0xFFFFu;
+            if (e == kMxNanScale) {                     // a block that is not finite counts as zeros, who sees it is told by nan_u
+              nan_u = min(nan_u, u0 + 2 * c + (i & 1) + 8 * (i >> 1));
+              ve[i / 2] &= i & 1 ? 0xFFFFu : 0xFFFF0000u;
+            } else {
+              most = max(most, (int)e);
+            }
+          }
+#pragma unroll
+          for (int sh = 1; sh < 4; sh <<= 1) {
+            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, sh));
+            low = min(low, __shfl_xor_sync(0xFFFFFFFFu, low, sh));
+          }
+          wide_v |= __any_sync(0xFFFFFFFFu, max(most, ov) > low + kDecValueWindow) != 0;
+          if (most > ov + kDecScaleAbove || ov == 0) {  // O's scale is set, or moves
+            if (ov != 0) {
+              const float down = pow2_at_most_15(ov - most);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i) o[nt][t][i] *= down;
+            }
+            ov = max(most, 1);
+          }
+          // (where they have differed too much already, only what O's scale minds)
+          least = (wide_v ? 0u : (uint32_t)(low - 1)) * 0x10001u;
+          passed = (uint32_t)(wide_v ? ov + kDecScaleAbove : min(ov + kDecScaleAbove, low + kDecValueWindow)) * 0x10001u;
+        }
+        if (__any_sync(0xFFFFFFFFu, keys_below)) {
+          if (wide_q || __any_sync(0xFFFFFFFFu, dec_key_below_f16<FMT, D>(at, lane, scale_word(0, lane)))) {       // the scores anew, of the values themselves
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[h][nt][e] = 0.f;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              uint32_t sw[2];
+              float none[4];
+#pragma unroll
+              for (int i = 0; i < 2; ++i) sw[i] = scale_word(0, g + 16 * h + 8 * i);
+              dec_scores_bf16<FMT, D, NT, false>(at, g + 16 * h, c, sw, [&](int nt, int j) {
+                const int r = first_row + 8 * nt + g;
+                if (8 * nt + g >= n_rows) return make_uint4(0, 0, 0, 0);
+                return load_input<true>(reinterpret_cast<const uint4*>(q + (long long)part.s * P.q_sb + (long long)(part.kv * P.group + r % P.group) * P.q_sh +
+                                                                       (long long)(r / P.group) * P.q_st + dec_column<FMT, D>(c, j)));
+              }, sc[h], none, none);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) sc[h][nt][e] *= P.scale * 1.4426950408889634f;
+            }
+            grow = see();
+          }
+        }
+        if (__any_sync(0xFFFFFFFFu, grow)) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -325,81 +423,72 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
 #pragma unroll
             for (int t = 0; t < TILES; ++t) { o[nt][t][e] *= alpha; o[nt][t][e + 2] *= alpha; }
           }
+        }
       }
-      uint32_t pf[2][NT][2];
+      // ---- weights, and O^T += V^T P^T, on fp16 operands or bf16 ones
+      const auto weigh = [&](auto is_wide) {
+        constexpr bool WIDE = decltype(is_wide)::value;
+        const auto pairs = [](uint32_t w, uint32_t factor2, auto& x) { if constexpr (WIDE) bf16_pairs<FMT>(w, factor2, x); else f16_pairs<FMT>(w, factor2, x); };
+        const auto mma = [](float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+          if constexpr (WIDE) mma_bf16(d, a0, a1, a2, a3, b0, b1); else mma_f16(d, a0, a1, a2, a3, b0, b1);
+        };
+        uint32_t pf[2][NT][2];
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) {
-        const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
+        for (int nt = 0; nt < NT; ++nt) {
+          const float m0 = m[nt][0] == -INFINITY ? 0.f : m[nt][0], m1 = m[nt][1] == -INFINITY ? 0.f : m[nt][1];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+          for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const float p0 = ex2(sc[h][nt][2 * i] - m0), p1 = ex2(sc[h][nt][2 * i + 1] - m1);
+              const uint32_t w = WIDE ? bf16x2(p0, p1) : f16x2(p0, p1);
+              const float2 back = WIDE ? make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u)) : __half22float2(*reinterpret_cast<const __half2*>(&w));
+              lx[nt][0] += p0;
+              lx[nt][1] += p1;
+              l[nt][0] += back.x;
+              l[nt][1] += back.y;
+              pf[h][nt][i] = transpose8x8(w);
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t f[2], v[4][VW];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            const float p0 = ex2(sc[h][nt][2 * i] - m0), p1 = ex2(sc[h][nt][2 * i + 1] - m1);
-            const uint32_t w = f16x2(p0, p1);
-            const float2 back = __half22float2(*reinterpret_cast<const __half2*>(&w));
-            lx[nt][0] += p0;
-            lx[nt][1] += p1;
-            l[nt][0] += back.x;
-            l[nt][1] += back.y;
-            pf[h][nt][i] = transpose8x8(w);
+            // 2^(e - ov) of both: exponent fields (zero for what is not there, and elements of zero)
+            const int bias = (WIDE ? 127 : 15) - ov;
+            f[i] = (uint32_t)__viaddmax_s16x2_relu(ve[2 * h + i], ((uint32_t)bias & 0xFFFFu) * 0x10001u, 0u) << (WIDE ? 7 : 10);
           }
-      }
-      // ---- O^T += V^T P^T
-      int e[8], most = 0;                              // scale bytes of the lane's eight keys in its block of columns
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int row = 2 * c + (i & 1) + 8 * (i >> 1);
-        e[i] = (int)(scale_word(128, row) >> (8 * (D == 128 ? g >> 1 : g >> 2)) & 0xFFu);
-        if (e[i] == (int)kMxNanScale) { nan_u = min(nan_u, u0 + row); e[i] = -200; }        // (becomes zeros)
-        most = max(most, e[i]);
-      }
-      if (__any_sync(0xFFFFFFFFu, most > ov + kDecScaleAbove || ov == 0)) {                // O's scale is set, or moves
-        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 1));
-        most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, 2));
-        if (most > ov + kDecScaleAbove || ov == 0) {
-          const float down = ov == 0 ? 0.f : pow2_at_most_15(ov - most);
-          ov = max(most, 1);
+          for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kTile + B::place(16 * h + 2 * c + (i & 1) + 8 * (i >> 1), g * B::kVBytes), v[i]);
 #pragma unroll
-          for (int nt = 0; nt < NT; ++nt)
+          for (int w = 0; w < VW; ++w) {
+            // the word's columns, the rows of a pair side by side: x those of keys 2 c and 2 c + 1, y 8 on
+            if constexpr (FMT == QUOKA_KV_MXFP8) {
 #pragma unroll
-            for (int t = 0; t < TILES; ++t)
+              for (int half = 0; half < 2; ++half) {
+                uint32_t x[2], y[2];
+                pairs(__byte_perm(v[0][w], v[1][w], half ? 0x7362 : 0x5140), f[0], x);
+                pairs(__byte_perm(v[2][w], v[3][w], half ? 0x7362 : 0x5140), f[1], y);
 #pragma unroll
-              for (int i = 0; i < 4; ++i) o[nt][t][i] *= down;
-        }
-      }
+                for (int nt = 0; nt < NT; ++nt) mma(o[nt][2 * w + half], x[0], x[1], y[0], y[1], pf[h][nt][0], pf[h][nt][1]);
+              }
+            } else {
+              constexpr uint32_t kLow = 0x0F0F0F0Fu;
+              uint32_t x0[4], x1[4], y0[4], y1[4];        // even columns, odd columns
+              pairs((v[0][w] & kLow) | (v[1][w] << 4 & ~kLow), f[0], x0);
+              pairs((v[0][w] >> 4 & kLow) | (v[1][w] & ~kLow), f[0], x1);
+              pairs((v[2][w] & kLow) | (v[3][w] << 4 & ~kLow), f[1], y0);
+              pairs((v[2][w] >> 4 & kLow) | (v[3][w] & ~kLow), f[1], y1);
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t f[2], v[4][VW];
+              for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) f[i] = f16x2(pow2_at_most_15(e[4 * h + 2 * i] - ov), pow2_at_most_15(e[4 * h + 2 * i + 1] - ov));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) lds_words<VW>(at + B::kTile + B::place(16 * h + 2 * c + (i & 1) + 8 * (i >> 1), g * B::kVBytes), v[i]);
-#pragma unroll
-        for (int w = 0; w < VW; ++w) {
-          // the word's columns, the rows of a pair side by side: x those of keys 2 c and 2 c + 1, y 8 on
-          if constexpr (FMT == QUOKA_KV_MXFP8) {
-#pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              uint32_t x[2], y[2];
-              f16_pairs<FMT>(__byte_perm(v[0][w], v[1][w], half ? 0x7362 : 0x5140), f[0], x);
-              f16_pairs<FMT>(__byte_perm(v[2][w], v[3][w], half ? 0x7362 : 0x5140), f[1], y);
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][2 * w + half], x[0], x[1], y[0], y[1], pf[h][nt][0], pf[h][nt][1]);
+                for (int nt = 0; nt < NT; ++nt) mma(o[nt][4 * w + i], x0[i], x1[i], y0[i], y1[i], pf[h][nt][0], pf[h][nt][1]);
             }
-          } else {
-            constexpr uint32_t kLow = 0x0F0F0F0Fu;
-            uint32_t x0[4], x1[4], y0[4], y1[4];        // even columns, odd columns
-            f16_pairs<FMT>((v[0][w] & kLow) | (v[1][w] << 4 & ~kLow), f[0], x0);
-            f16_pairs<FMT>((v[0][w] >> 4 & kLow) | (v[1][w] & ~kLow), f[0], x1);
-            f16_pairs<FMT>((v[2][w] & kLow) | (v[3][w] << 4 & ~kLow), f[1], y0);
-            f16_pairs<FMT>((v[2][w] >> 4 & kLow) | (v[3][w] & ~kLow), f[1], y1);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-              for (int nt = 0; nt < NT; ++nt) mma_f16(o[nt][4 * w + i], x0[i], x1[i], y0[i], y1[i], pf[h][nt][0], pf[h][nt][1]);
           }
         }
-      }
+      };
+      if (wide_v) weigh(std::true_type{}); else weigh(std::false_type{});
       __syncwarp();                                    // the scale words of this stage have been read
       fill(stage);
       if (++stage == ST) { stage = 0; phase ^= 1; }

@@ -73,12 +73,123 @@ __device__ __forceinline__ void f16_pairs(uint32_t w, uint32_t factor2, uint32_t
 #pragma unroll
   for (int i = 0; i < N; ++i) o[i] = mul_f16x2(o[i], factor2);
 }
-// 2^diff, diff <= 15, as an fp16 number (zero below its range).
-__device__ __forceinline__ float pow2_at_most_15(int diff) { return __uint_as_float((uint32_t)(max(diff, -60) + 127) << 23); }
+// The same as bf16 pairs, whatever the scale.
+template <int FMT, int N>
+__device__ __forceinline__ void bf16_pairs(uint32_t w, uint32_t factor2, uint32_t (&o)[N]) {
+  uint32_t x[4];
+  mx_bits_bf16x8<FMT>(w, 0u, x);
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = mul_bf16x2(mul_bf16x2(x[i], FMT == QUOKA_KV_MXFP8 ? 0x7B807B80u : 0x7E807E80u), factor2);
+}
+__device__ __forceinline__ void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// 2^diff, -126 <= diff <= 15 (below: 2^-126).
+__device__ __forceinline__ float pow2_at_most_15(int diff) { return __uint_as_float((uint32_t)(max(diff, -126) + 127) << 23); }
+
+// ---- What fp16 operands hold, and what is done where they do not.
+// A key's row goes into the product divided by its largest block's scale: elements of a block that is kDecKeyWindow powers of two below it
+// are fp16 numbers still (multiples of 2^-9 or 2^-1; fp16's are multiples of 2^-24).  A row with a block below that, of elements that are not all
+// zero, and a query whose smallest element fp16 does not hold beside its largest one, take bf16 products of the values as they are
+// (dec_scores_bf16): exact, as those of a bf16 cache, for three times the instructions.
+template <int FMT>
+constexpr int kDecKeyWindow = FMT == QUOKA_KV_MXFP8 ? 15 : 23;
+// Columns of a query row, 8 at a time, that go with a lane's pieces of key rows.
+template <int FMT, int D>
+__device__ __forceinline__ int dec_column(int c, int j) { return FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j; }
+// Magnitudes of a query row's elements, pairs of bf16 bits: the largest, and one less than the smallest but zero (by halves of a word).
+struct DecMagnitudes {
+  uint32_t most = 0u, low = 0xFFFFFFFFu;
+  __device__ __forceinline__ void take(uint32_t x) {
+    const uint32_t m = x & 0x7FFF7FFFu;
+    most = __vmaxu2(most, m);
+    low = __viaddmin_u16x2(m, 0xFFFFFFFFu, low);
+  }
+  // bits of the largest, as a float's
+  __device__ __forceinline__ uint32_t largest() const { return max(most & 0xFFFF0000u, most << 16); }
+  // whether the smallest, times 2^up, has its last bit below 2^-24 (a number with exponent field e ends at 2^(max(e, 1) - 134))
+  __device__ __forceinline__ bool below_f16(int up) const {
+    const int from = 110 - up;
+    return from > 1 && (int)min(low & 0xFFFFu, low >> 16) + 1 < (from << 7);
+  }
+};
+// Whether the factors 2^diff of a lane's pieces of keys, fp16 pairs, have one of a block that far below its row's largest.
+struct DecFactors {
+  uint32_t least = 0xFFFFFFFFu;
+  __device__ __forceinline__ void take(uint32_t f) { least = __vminu2(least, f); }
+  template <int FMT>
+  __device__ __forceinline__ bool below_f16() const { return (least & 0xFFFFu) < (FMT == QUOKA_KV_MXFP8 ? 0x0200u : 0x0002u); }      // 2^-kDecKeyWindow
+};
+// Whether key row `row` of the tile at `at` (scale word sw) has such a block, not zero.
+template <int FMT, int D>
+__device__ __forceinline__ bool dec_key_below_f16(uint32_t at, int row, uint32_t sw) {
+  uint32_t top = __vmaxu4(sw, sw >> 16);
+  top = max(top & 0xFFu, top >> 8 & 0xFFu);
+  if (top == kMxNanScale) return false;
+  bool below = false;
+#pragma unroll 1
+  for (int b = 0; b < D / kMxBlock; ++b) {
+    if ((int)(sw >> (8 * b) & 0xFFu) >= (int)top - kDecKeyWindow<FMT>) continue;
+    uint32_t any = 0;
+#pragma unroll 1
+    for (int i = 0; i < 4 * kMxBits<FMT>; i += 16) {   // 16 bytes: whole chunks of the swizzle
+      uint32_t w[4];
+      lds_words<4>(at + DecBytes<FMT, D>::place(row, 4 * kMxBits<FMT> * b + i), w);
+      any |= w[0] | w[1] | w[2] | w[3];
+    }
+    below |= (any & (FMT == QUOKA_KV_MXFP8 ? 0x7F7F7F7Fu : 0x77777777u)) != 0;
+  }
+  return below;
+}
+// Products of 16 keys (rows row0 and row0 + 8 of the tile at `at` are this lane's, with scale words sw) and 8 NT query rows, bf16: sc, and of
+// the keys with themselves, where NORM.  load_q(nt, j): the lane's 8 columns of its query row.  A block that is not finite makes its key's NaN.
+template <int FMT, int D, int NT, bool NORM, typename LoadQ>
+__device__ __forceinline__ void dec_scores_bf16(uint32_t at, int row0, int c, const uint32_t (&sw)[2], LoadQ&& load_q, float (&sc)[NT][4], float (&na)[4],
+                                                float (&nb)[4]) {
+  typedef DecBytes<FMT, D> B;
+  const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
+#pragma unroll 1                                       // (few instructions: hardly ever taken)
+  for (int j = 0; j < D / 32; ++j) {
+    const int p = j * kMxBits<FMT> / B::kKBytes, within = j * kMxBits<FMT> % B::kKBytes;
+    uint32_t k[2][4];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      uint32_t w[2] = {0u, 0u};
+      lds_words<kMxBits<FMT> / 4>(at + B::place(row0 + 8 * i, c * B::kKBytes + 64 * p) + within, w);
+      const uint32_t f = mx_scale_bf16x2(sw[i] >> (8 * (blk + 2 * p)) & 0xFFu);
+      mx_bits_bf16x8<FMT>(w[0], w[1], k[i]);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) k[i][e] = mul_bf16x2(mul_bf16x2(k[i][e], FMT == QUOKA_KV_MXFP8 ? 0x7B807B80u : 0x7E807E80u), f);
+    }
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const uint4 q = load_q(nt, j);
+      mma_bf16(sc[nt], k[0][0], k[1][0], k[0][1], k[1][1], q.x, q.y);
+      mma_bf16(sc[nt], k[0][2], k[1][2], k[0][3], k[1][3], q.z, q.w);
+    }
+    if constexpr (NORM) {
+#pragma unroll
+      for (int e = 0; e < 4; e += 2) {
+        mma_bf16(na, k[0][e], k[1][e], k[0][e + 1], k[1][e + 1], k[0][e], k[0][e + 1]);
+        mma_bf16(nb, k[0][e], k[1][e], k[0][e + 1], k[1][e + 1], k[1][e], k[1][e + 1]);
+      }
+    }
+  }
+}
 // Weight of a result with the reference point m among results whose largest is mx: what has seen nothing weighs nothing.
 __device__ __forceinline__ float dec_weight(float m, float mx) { return m == mx ? 1.f : m == -INFINITY ? 0.f : ex2(m - mx); }
 constexpr int kDecMaxAbove = 15, kDecHeadroom = 7;       // of a weight's exponent over the reference point, at most and when it is set
 constexpr int kDecScaleAbove = 7;                        // of a value block's exponent over O's: 448 * 2^7 is an fp16 number
+// Of the largest over the smallest exponent of value blocks that fp16 weights and values are used for.  It keeps the values exact (their
+// exponents are 9 below O's at most), and weights that fp16 does not hold, 2^-32 of the largest one and less, from mattering: 2^-23 of the
+// output for each of them.
+constexpr int kDecValueWindow = 9;
 
 __device__ __forceinline__ uint32_t transpose8x8(uint32_t v) {
   uint32_t r;

@@ -91,6 +91,7 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
   grid_dependency_wait();                             // Q-bar comes from the kernel before
   uint32_t qf[2 * KSTEPS];
   float qs[2] = {0.f, 0.f};
+  bool wide_q = false;                                // a query has elements that fp16 does not hold beside its largest one
   int stage = 0, s_cur = -1, kv_cur = -1, gr = part.begin + warp;
   uint32_t phase = 0;
   bool ok = true;
@@ -105,19 +106,20 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
       s_cur = part.s; kv_cur = part.kv;
       const __nv_bfloat16* qr = qbar + (((long long)part.s * P.n_kv + part.kv) * P.n_sel + min(g, P.n_sel - 1)) * D;
       uint4 w[D / 32];
-      uint32_t top = 0;
+      DecMagnitudes mags;
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
-        const int col = FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j;
-        w[j] = __ldcg(reinterpret_cast<const uint4*>(qr + col));
+        w[j] = __ldcg(reinterpret_cast<const uint4*>(qr + dec_column<FMT, D>(c, j)));
         if (g >= P.n_sel) w[j] = make_uint4(0, 0, 0, 0);
         const uint32_t x[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) top = max(top, max(x[i] << 16 & 0x7FFF0000u, x[i] & 0x7FFF0000u));
+        for (int i = 0; i < 4; ++i) mags.take(x[i]);
       }
+      uint32_t top = mags.largest();
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
       top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       const int up = min(14 + 127 - (int)(top >> 23), 120);
+      wide_q = __any_sync(0xFFFFFFFFu, mags.below_f16(up));
       const float f = __uint_as_float((uint32_t)(127 + up) << 23), back = __uint_as_float((uint32_t)(127 - up) << 23);
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
@@ -135,54 +137,22 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
       if (!mbar_wait_done(&landed[stage], phase, wc)) { ok = false; break; }
       __syncwarp();
       const uint32_t at = ring + (uint32_t)stage * B::kTile, meta = metas + (uint32_t)stage * kFewMeta<FMT, D>;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        float sc[4] = {0.f, 0.f, 0.f, 0.f}, na[4] = {0.f, 0.f, 0.f, 0.f}, nb[4] = {0.f, 0.f, 0.f, 0.f};
-        uint32_t w[2][KW], f[2][B::kKPieces], bad[2];
-        float key[2], inv[2];
+      const auto row_scales = [&](int row) {
+        uint32_t sw;
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sw) : "r"(meta + 4 * row) : "memory");
+        if (D == 64) {
+          uint32_t shift;
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 256 + 4 * row) : "memory");
+          sw = sw >> shift & 0xFFFFu;
+        }
+        return sw;
+      };
+      // Scores of 16 keys from their products with queries 2 c and 2 c + 1 (rows g, g + 8), and with themselves.
+      const auto write = [&](int h, const float (&sc)[4], const float (&na)[4], const float (&nb)[4], const float (&key)[2], const float (&inv)[2],
+                             const bool (&bad)[2]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int row = g + 16 * h + 8 * i;
-#pragma unroll
-          for (int p = 0; p < B::kKPieces; ++p) lds_words<B::kKBytes / 4>(at + B::place(row, c * B::kKBytes + 64 * p), w[i] + p * (B::kKBytes / 4));
-          uint32_t sw;
-          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(sw) : "r"(meta + 4 * row) : "memory");
-          if (D == 64) {
-            uint32_t shift;
-            asm volatile("ld.shared.u32 %0, [%1];" : "=r"(shift) : "r"(meta + 256 + 4 * row) : "memory");
-            sw = sw >> shift & 0xFFFFu;
-          }
-          inv[i] = 1.f;
-          if (cached) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(inv[i]) : "r"(meta + 128 + 4 * row) : "memory");
-          uint32_t top = __vmaxu4(sw, sw >> 16);       // the largest of the row's scale bytes
-          top = max(top & 0xFFu, top >> 8 & 0xFFu);
-          bad[i] = top == kMxNanScale;
-          key[i] = mx_scale(top);
-          const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
-#pragma unroll
-          for (int p = 0; p < B::kKPieces; ++p) {
-            const float x = pow2_at_most_15((int)(sw >> (8 * (blk + 2 * p)) & 0xFFu) - (int)top);
-            f[i][p] = f16x2(x, x);
-          }
-        }
-#pragma unroll
-        for (int j = 0; j < KW; ++j) {
-          constexpr int N = FMT == QUOKA_KV_MXFP8 ? 2 : 4;
-          uint32_t a[N], b[N];
-          f16_pairs<FMT>(w[0][j], f[0][j / (KW / B::kKPieces)], a);
-          f16_pairs<FMT>(w[1][j], f[1][j / (KW / B::kKPieces)], b);
-#pragma unroll
-          for (int i = 0; i < N / 2; ++i) {
-            mma_f16(sc, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], qf[N * j + 2 * i], qf[N * j + 2 * i + 1]);
-            if constexpr (OWN_NORM) {                  // keys 0-7 of the 16 against all, and 8-15
-              mma_f16(na, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], a[2 * i], a[2 * i + 1]);
-              mma_f16(nb, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], b[2 * i], b[2 * i + 1]);
-            }
-          }
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {                   // keys g and g + 8: of queries 2 c and 2 c + 1 in this lane
-          const float s0 = sc[2 * i] * qs[0], s1 = sc[2 * i + 1] * qs[1];
+          const float s0 = sc[2 * i], s1 = sc[2 * i + 1];
           float v;
           if (P.agg_mean) {                             // (queries past the retained ones score zero)
             v = s0 + s1;
@@ -204,6 +174,80 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
           if (bad[i] && !P.agg_mean) v = -INFINITY;
           const int t = gr * kDecGranule + 16 * h + 8 * i + g;
           if (c == g >> 1 && t < part.lens.cnt) out[t] = v;
+        }
+      };
+      const auto norms_kept = [&](int row) {
+        float inv = 1.f;
+        if (cached) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(inv) : "r"(meta + 128 + 4 * row) : "memory");
+        return inv;
+      };
+      DecFactors factors;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        float sc[4] = {0.f, 0.f, 0.f, 0.f}, na[4] = {0.f, 0.f, 0.f, 0.f}, nb[4] = {0.f, 0.f, 0.f, 0.f};
+        uint32_t w[2][KW], f[2][B::kKPieces];
+        bool bad[2];
+        float key[2], inv[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int row = g + 16 * h + 8 * i;
+#pragma unroll
+          for (int p = 0; p < B::kKPieces; ++p) lds_words<B::kKBytes / 4>(at + B::place(row, c * B::kKBytes + 64 * p), w[i] + p * (B::kKBytes / 4));
+          const uint32_t sw = row_scales(row);
+          inv[i] = norms_kept(row);
+          uint32_t top = __vmaxu4(sw, sw >> 16);       // the largest of the row's scale bytes
+          top = max(top & 0xFFu, top >> 8 & 0xFFu);
+          bad[i] = top == kMxNanScale;
+          key[i] = mx_scale(top);
+          const int blk = FMT == QUOKA_KV_MXFP4 && D == 128 ? c : c >> 1;
+#pragma unroll
+          for (int p = 0; p < B::kKPieces; ++p) {
+            const float x = pow2_at_most_15((int)(sw >> (8 * (blk + 2 * p)) & 0xFFu) - (int)top);
+            f[i][p] = f16x2(x, x);
+            factors.take(f[i][p]);
+          }
+        }
+#pragma unroll
+        for (int j = 0; j < KW; ++j) {
+          constexpr int N = FMT == QUOKA_KV_MXFP8 ? 2 : 4;
+          uint32_t a[N], b[N];
+          f16_pairs<FMT>(w[0][j], f[0][j / (KW / B::kKPieces)], a);
+          f16_pairs<FMT>(w[1][j], f[1][j / (KW / B::kKPieces)], b);
+#pragma unroll
+          for (int i = 0; i < N / 2; ++i) {
+            mma_f16(sc, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], qf[N * j + 2 * i], qf[N * j + 2 * i + 1]);
+            if constexpr (OWN_NORM) {                  // keys 0-7 of the 16 against all, and 8-15
+              mma_f16(na, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], a[2 * i], a[2 * i + 1]);
+              mma_f16(nb, a[2 * i], b[2 * i], a[2 * i + 1], b[2 * i + 1], b[2 * i], b[2 * i + 1]);
+            }
+          }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sc[e] *= qs[e & 1];
+        write(h, sc, na, nb, key, inv, bad);
+      }
+      // Where fp16 operands do not hold the granule: anew, of the values themselves, over what was written.
+      const bool below = factors.below_f16<FMT>();
+      if (__any_sync(0xFFFFFFFFu, below || wide_q)) {
+        if (wide_q || __any_sync(0xFFFFFFFFu, dec_key_below_f16<FMT, D>(at, lane, row_scales(lane)))) {
+#pragma unroll 1
+          for (int h = 0; h < 2; ++h) {
+            float sc[1][4] = {{0.f, 0.f, 0.f, 0.f}}, na[4] = {0.f, 0.f, 0.f, 0.f}, nb[4] = {0.f, 0.f, 0.f, 0.f};
+            uint32_t sw[2];
+            bool bad[2];
+            float key[2] = {1.f, 1.f}, inv[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              sw[i] = row_scales(g + 16 * h + 8 * i);
+              inv[i] = norms_kept(g + 16 * h + 8 * i);
+              bad[i] = __vcmpeq4(sw[i], 0xFFFFFFFFu) != 0u;
+            }
+            dec_scores_bf16<FMT, D, 1, OWN_NORM>(at, g + 16 * h, c, sw, [&](int, int j) {
+              if (g >= P.n_sel) return make_uint4(0, 0, 0, 0);
+              return __ldcg(reinterpret_cast<const uint4*>(qbar + (((long long)part.s * P.n_kv + part.kv) * P.n_sel + g) * D + dec_column<FMT, D>(c, j)));
+            }, sc, na, nb);
+            write(h, sc[0], na, nb, key, inv, bad);
+          }
         }
       }
       __syncwarp();                                    // the scale words of this stage have been read
