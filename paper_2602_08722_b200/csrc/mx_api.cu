@@ -167,6 +167,7 @@ quoka_status quoka_prefill_chunk_mx(const quoka_params* p, const quoka_mx_cache*
   if (st != QUOKA_OK) return st;
   if (!q || !k_cache || !v_cache || !out) return QUOKA_ERR_INVALID_ARG;
   if (!aligned16(q) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(out)) return QUOKA_ERR_INVALID_ARG;
+  if (p->impl == QUOKA_IMPL_TENSOR && ((p->max_ctx_len > 0 && !score_keys_mx_tc_supported(p)) || !attn_mx_tc_supported(p))) return QUOKA_ERR_UNSUPPORTED;
   if ((st = check_ws_mx(p, ws, ws_bytes)) != QUOKA_OK) return st;
   cudaStream_t cs = static_cast<cudaStream_t>(stream);
   const MxAttn a = plan_attn_mx(p, ws, ws_bytes, /*listed=*/true);
