@@ -255,10 +255,13 @@ int attn_same_plan_up_to(const quoka_params* p, int chunk) {
 
 bool attn_tc_supported(const quoka_params* p) {
   if (p->dtype != QUOKA_BF16) return false;
-  // the loaders address cache rows in 32-bit units of 16 bytes
-  const int64_t extent = (p->page_size ? p->kv_rows : (int64_t)p->batch) * p->kv_stride_b;
-  if (extent / 8 >= (int64_t)0xFFFFFFFFll) return false;
-  return true;
+  return kv_places_fit(p, 8);                         // the loaders address cache rows in 32-bit units of 16 bytes
+}
+bool kv_places_fit(const quoka_params* p, int unit) {
+  typedef __int128 Wide;                              // (nothing bounds the strides that a caller may give)
+  const Wide pages = p->page_size ? p->kv_rows : p->batch, rows = p->page_size ? kPage : p->kv_rows;
+  const Wide elements = (pages - 1) * p->kv_stride_b + (Wide)(p->n_kv_heads - 1) * p->kv_stride_h + (rows - 1) * p->kv_stride_t + p->head_dim;
+  return elements / unit < (Wide)0xFFFFFFFFll;
 }
 
 bool encode_q_tensor_map(CUtensorMap* out, const DevParams& P, const void* q) {

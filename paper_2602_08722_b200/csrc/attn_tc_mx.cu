@@ -11,9 +11,8 @@ AttnKernel pick_attn_mx4(bool pair, int d, bool sparse, bool parts, bool in_clus
 bool attn_mx_tc_supported(const quoka_params* p) {
   if (p->dtype != QUOKA_BF16) return false;
   // the loaders count cache rows, and units of 16 elements, in 32 bits
-  const int64_t extent = (p->page_size ? p->kv_rows : (int64_t)p->batch) * p->kv_stride_b;
   const int64_t rows = (p->page_size ? p->kv_rows * kPage : (int64_t)p->batch * p->kv_rows) * p->n_kv_heads;
-  return extent / 16 < (int64_t)0xFFFFFFFFll && rows < (int64_t)0xFFFFFFFFll;
+  return kv_places_fit(p, 16) && rows < (int64_t)0xFFFFFFFFll;
 }
 
 template <bool PAIR, bool WIDE, bool FP8>

@@ -25,6 +25,8 @@ size_t attn_plan_scratch_bytes(const quoka_params* p, const AttnPlan& plan);
 size_t attn_split_partial_bytes(const quoka_params* p, const AttnPlan& plan);
 size_t attn_split_counter_bytes(const quoka_params* p, const AttnPlan& plan);
 bool attn_tc_supported(const quoka_params* p);
+// Whether 32 bits count the cache's units of `unit` elements up to its last element's, wherever the strides put it.
+bool kv_places_fit(const quoka_params* p, int unit);
 // Whether the attention grid (256 query rows per CTA) has fewer CTAs than the GPU has SMs.
 bool attn_below_a_wave(const quoka_params* p);
 // Whether it is small enough for a plan with parts
