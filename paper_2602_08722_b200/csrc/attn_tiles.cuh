@@ -486,6 +486,10 @@ __device__ __forceinline__ void attn_mark_nan(uint32_t (&r)[32], const int* v_na
     }
   }
 }
+// Whether a part's output is added up: over a microscaled cache, or rows unpacked from one, also where its keys weigh nothing beside the others',
+// as it may be marked as not finite.
+template <int FMT>
+__device__ __forceinline__ bool part_counts(bool seen, float weight) { return FMT != 0 ? seen : weight != 0.f; }
 template <int D, int FMT = 0>
 __device__ __forceinline__ void attn_store_row(const DevParams& P, uint32_t o_addr, float m_run, float l_run, int s, int h,
                                                int row, bool store, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
@@ -565,9 +569,10 @@ __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job,
     float l = 0.f;
 #pragma unroll
     for (int q = 0; q < 8; ++q) {
-      const float w = wgt[q] == -INFINITY ? 0.f : ex2(wgt[q] - M);
+      const bool seen = wgt[q] != -INFINITY;
+      const float w = seen ? ex2(wgt[q] - M) : 0.f;
       if (q < n_parts) l += w * __ldcg(tile0 + (size_t)q * 2 * kTile + (D + 1) * 128 + row_in_tile);
-      wgt[q] = w;
+      wgt[q] = part_counts<FMT>(seen, w) ? w : -1.f;
     }
     const float inv = attn_inverse<FMT>(l);
     __nv_bfloat16* orow = out + (long long)s * P.o_sb + (long long)h * P.o_sh + (long long)row * P.o_st;
@@ -578,7 +583,7 @@ __device__ __forceinline__ void attn_split_epilogue(const DevParams& P, int job,
       for (int i = 0; i < 32; ++i) acc[i] = 0.f;
 #pragma unroll
       for (int q = 0; q < 8; ++q) {
-        if (q < n_parts && wgt[q] != 0.f) {
+        if (q < n_parts && wgt[q] >= 0.f) {
           const float* src = tile0 + (size_t)q * 2 * kTile + (c * 32) * 128 + row_in_tile;
 #pragma unroll
           for (int i = 0; i < 32; ++i) acc[i] = fmaf(wgt[q], __ldcg(src + i * 128), acc[i]);
@@ -657,12 +662,13 @@ __device__ __forceinline__ void attn_merge_cluster(const DevParams& P, unsigned 
     for (int o = 4; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
     M = __shfl_sync(0xFFFFFFFFu, M, 0);
     const float wgt = m == -INFINITY ? 0.f : ex2(m - M);
+    const uint32_t counts = __ballot_sync(0xFFFFFFFFu, part_counts<FMT>(m != -INFINITY, wgt));
     float L = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
     for (int p = 0; p < kMaxParts; ++p) {                                       // (lanes past the parts hold a weight of 0)
       const float w = __shfl_sync(0xFFFFFFFFu, wgt, p);
-      const float4 o = w != 0.f ? v[p] : make_float4(0.f, 0.f, 0.f, 0.f);
+      const float4 o = (counts >> p & 1u) != 0u ? v[p] : make_float4(0.f, 0.f, 0.f, 0.f);
       L = fmaf(w, __shfl_sync(0xFFFFFFFFu, l, p), L);
       acc.x = fmaf(w, o.x, acc.x); acc.y = fmaf(w, o.y, acc.y);
       acc.z = fmaf(w, o.z, acc.z); acc.w = fmaf(w, o.w, acc.w);
