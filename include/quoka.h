@@ -261,8 +261,9 @@ quoka_status quoka_prefill_chunk_static(const quoka_params* p, const void* q, co
  * quoka_append_kv_mx picks the smallest e with (largest magnitude of the block) <= M * 2^e, M = 448 or 6, limited to -64 <= e <= 15,
  * writes b = e + 127 and the values times 2^-e rounded to nearest, ties to even (beyond M * 2^15 = 14680064 or 196608 they
  * saturate).  A block with a value that is not finite gets b = 255 and elements of zero, and reads as NaN throughout.
- * Scales outside 63 .. 142 other than 255 (a cache that other code wrote) are read by quoka_read_kv_mx and the scalar kernels
- * (impl = QUOKA_IMPL_SIMT) only; elsewhere their values are undefined.
+ * What it does not write, scales outside 63 .. 142 other than 255, and e4m3's codes of NaN (0x7F and 0xFF, which read as NaN), is read by
+ * quoka_read_kv_mx and the scalar kernels (impl = QUOKA_IMPL_SIMT) only; elsewhere the results of a call that reads such a row are undefined.
+ * (A cache that other code wrote marks what is not finite by a scale of 255.)
  *
  * Every value of such a cache is a bf16 number exactly: attention and scores are those of a bf16 cache that holds the values
  * quoka_read_kv_mx returns.  Products are exact and added up in fp32.  Softmax weights are bf16; calls of a few query rows (see

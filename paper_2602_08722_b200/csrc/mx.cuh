@@ -22,12 +22,18 @@ constexpr bool kIsMx = FMT == QUOKA_KV_MXFP8 || FMT == QUOKA_KV_MXFP4;
 template <int FMT>
 constexpr int kMxBits = FMT == QUOKA_KV_MXFP8 ? 8 : 4;
 
+// e4m3's codes 0x7F and 0xFF are no numbers.  quoka_append_kv_mx does not write them; reading back and the scalar kernels give NaN for them,
+// the others take them for whatever their conversion makes of the bits.
+constexpr uint32_t kE4m3Nan = 0x7Fu;
+// Whether a word of four codes has one.
+__device__ __forceinline__ bool e4m3_has_nan(uint32_t w) { return (((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) != 0u; }
+
 // The value of an element: its bits at the place of an fp32 number's exponent and fraction are the value times a power of two
 // (subnormals too), which the multiplication takes off.
 template <int FMT>
 __device__ __forceinline__ float mx_element(uint32_t code) {
   if constexpr (FMT == QUOKA_KV_MXFP8)
-    return __uint_as_float((code & 0x80u) << 24 | (code & 0x7Fu) << 20) * 0x1p120f;
+    return (code & 0x7Fu) == kE4m3Nan ? __uint_as_float(0x7FC00000u) : __uint_as_float((code & 0x80u) << 24 | (code & 0x7Fu) << 20) * 0x1p120f;
   else
     return __uint_as_float((code & 8u) << 28 | (code & 7u) << 22) * 0x1p126f;
 }

@@ -167,7 +167,16 @@ __device__ __forceinline__ void store_values(E* p, const uint2& w, uint32_t scal
     reinterpret_cast<float4*>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4*>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
   } else {
-    *reinterpret_cast<uint4*>(p) = mx_values_bf16x8<FMT>(w.x, w.y, mx_scale_bf16x2(scale));
+    uint4 v = mx_values_bf16x8<FMT>(w.x, w.y, mx_scale_bf16x2(scale));
+    if constexpr (FMT == QUOKA_KV_MXFP8) {
+      if (e4m3_has_nan(w.x) || e4m3_has_nan(w.y)) {     // (a cache that other code wrote)
+        const auto pair = [](uint32_t x, uint32_t codes) {
+          return ((codes & 0x7Fu) == kE4m3Nan ? 0x7FC0u : x & 0xFFFFu) | ((codes >> 8 & 0x7Fu) == kE4m3Nan ? 0x7FC00000u : x & 0xFFFF0000u);
+        };
+        v = make_uint4(pair(v.x, w.x), pair(v.y, w.x >> 16), pair(v.z, w.y), pair(v.w, w.y >> 16));
+      }
+    }
+    *reinterpret_cast<uint4*>(p) = v;
   }
 }
 
