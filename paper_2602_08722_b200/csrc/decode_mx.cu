@@ -21,7 +21,8 @@
 // 2^31 below its largest, blocks of values 2^9 below the largest of their columns.  Where a granule of 32 keys has others, and only there, its
 // scores or its weighted values are taken from bf16 operands, which hold every value of a cache: so what a key of no weight, or one that a row
 // does not see, is worth has no part in the row's rounding.  Weights are fp16 otherwise; those 2^-32 times the largest and less then vanish, against
-// values 2^9 times the others' at most.  To look for such granules takes 2 % of the time (135.7 us where the kernel without took 132.4, sixteen long sequences).
+// values 2^9 times the others' at most.  To look for such granules takes 1 % of the time (sixteen long sequences in a warm loop: 133.9 us, without 132.2), with the code
+// for them out of line (in line 135.7).
 //
 // Split: units are (sequence, KV head, row group).  Few keys: a CTA per unit, or a cluster of CTAs with an equal share of the unit's granules of
 // 32 keys each, whose results are added up through distributed shared memory.  Else the granules of all units are one list, cut into equal contiguous
@@ -343,7 +344,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
       // ---- do fp16 operands hold the granule, and the reference point: one vote, rarely with something to do
       const bool keys_below = factors.below_f16<FMT>() || wide_q;
       bool grow = see();
-      if (__any_sync(0xFFFFFFFFu, grow || keys_below || !values_met)) {
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, grow || keys_below || !values_met), 0)) {
         if (__any_sync(0xFFFFFFFFu, !values_met)) {
           int most = 0, low = (int)(ve_low & 0xFFFFu) + 1;
           low = min(low, (int)(ve_low >> 16) + 1);
@@ -379,7 +380,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
           least = (wide_v ? 0u : (uint32_t)(low - 1)) * 0x10001u;
           passed = (uint32_t)(wide_v ? ov + kDecScaleAbove : min(ov + kDecScaleAbove, low + kDecValueWindow)) * 0x10001u;
         }
-        if (__any_sync(0xFFFFFFFFu, keys_below)) {
+        if (__builtin_expect(__any_sync(0xFFFFFFFFu, keys_below), 0)) {
           if (wide_q || __any_sync(0xFFFFFFFFu, dec_key_below_f16<FMT, D>(at, lane, scale_word(0, lane)))) {       // the scores anew, of the values themselves
 #pragma unroll
             for (int h = 0; h < 2; ++h)
@@ -488,7 +489,7 @@ decode_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__ q,
           }
         }
       };
-      if (wide_v) weigh(std::true_type{}); else weigh(std::false_type{});
+      if (__builtin_expect(!wide_v, 1)) weigh(std::false_type{}); else weigh(std::true_type{});
       __syncwarp();                                    // the scale words of this stage have been read
       fill(stage);
       if (++stage == ST) { stage = 0; phase ^= 1; }

@@ -228,7 +228,7 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
       }
       // Where fp16 operands do not hold the granule: anew, of the values themselves, over what was written.
       const bool below = factors.below_f16<FMT>();
-      if (__any_sync(0xFFFFFFFFu, below || wide_q)) {
+      if (__builtin_expect(__any_sync(0xFFFFFFFFu, below || wide_q), 0)) {
         if (wide_q || __any_sync(0xFFFFFFFFu, dec_key_below_f16<FMT, D>(at, lane, row_scales(lane)))) {
 #pragma unroll 1
           for (int h = 0; h < 2; ++h) {
