@@ -40,7 +40,9 @@ static quoka_status run_score_keys_mx(const quoka_params* p, const quoka_mx_cach
 }
 
 // The scratch of a few query rows' attention comes last and has to be there; that of unpacked rows comes last too and may be missing.
-static size_t scratch_mx(const quoka_params* p) { return p->dtype == QUOKA_BF16 && decode_mx_applies(p) ? decode_mx_scratch_bytes(p) : 0; }
+static size_t scratch_mx(const quoka_params* p) {
+  return p->impl == QUOKA_IMPL_AUTO && p->dtype == QUOKA_BF16 && decode_mx_applies(p) ? decode_mx_scratch_bytes(p) : 0;
+}
 static quoka_status check_ws_mx(const quoka_params* p, void* ws, size_t ws_bytes) {
   const quoka_status st = check_ws(p, ws, ws_bytes);
   if (st != QUOKA_OK) return st;

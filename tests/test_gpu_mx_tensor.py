@@ -85,3 +85,18 @@ def test_a_refused_fused_call_launches_nothing(fmt):
         api.quoka_prefill_chunk_mx(P.p, P.mx, P.q, P.k, P.v, P.out, None, None, P.ws)
     assert e.value.status == api.ERR_UNSUPPORTED and api.quoka_launch_count() == before
     assert (P.out == 7.0).all()
+
+
+@pytest.mark.parametrize("impl", [api.IMPL_SIMT, api.IMPL_TENSOR])
+@pytest.mark.parametrize("n_q,n_kv,d,C", [(8, 2, 128, 1), (8, 1, 64, 5)])
+def test_other_kernels_than_the_few_row_ones_do_not_need_their_scratch(impl, n_q, n_kv, d, C):
+    """The bf16 call's workspace is enough, and nothing behind it is written."""
+    inp = synth.make_chunk_inputs(95, 1, n_q, n_kv, d, [2500], C, "bf16")
+    P = R.MxProblem(inp, api.KV_MXFP8, n_retain=4, kv_budget=300, impl=impl)
+    n = api.quoka_workspace_size(P.p)
+    ws = torch.full((n + (1 << 22),), 0xA5, dtype=torch.uint8, device="cuda")
+    ws[:256] = 0
+    api.quoka_dense_chunk_attn_mx(P.p, P.mx, P.q, P.k, P.v, P.out, None, ws[:n])
+    PA.check_attention(PA.f64(P.out[0]), P.reference(0)[0], "bf16")
+    api.quoka_prefill_chunk_mx(P.p, P.mx, P.q, P.k, P.v, P.out, None, None, ws[:n])
+    assert api.quoka_last_device_status(ws) == 0 and (ws[n:] == 0xA5).all()
