@@ -285,8 +285,8 @@ typedef struct {
 
 /* Workspace of the calls below, in the manner of quoka_workspace_size: at least quoka_workspace_size's bytes, of which the split
  * kernel's may be missing as there, except that calls of a few bf16 query rows (chunk_len * n_Q / n_KV <= 32 with 128 columns, <= 40 with 64;
- * chunk_len 1) with impl = QUOKA_IMPL_AUTO need theirs.  For 2048 query rows per KV head or more it has room, 256 MiB at most, for the rows attended to as bf16; this comes last, and
- * calls without it convert rows as they go. */
+ * chunk_len 1) with impl = QUOKA_IMPL_AUTO need theirs.  For 2048 query rows per KV head or more (8192 in dense calls of 128 columns) it has room,
+ * 256 MiB at most, for the rows attended to as bf16; this comes last, and calls without it convert rows as they go. */
 quoka_status quoka_workspace_size_mx(const quoka_params* p, const quoka_mx_cache* mx, size_t* bytes);
 
 /* quoka_append_kv into a microscaled cache: k_new, v_new dense [b][n_KV][C][d] of `dtype`.  k_inv_norm, where not NULL, gets the

@@ -1,6 +1,7 @@
-// Loader warps of the tensor-core attention kernels over a microscaled cache: rows of 8- or 4-bit elements come in through
-// registers, become bf16 there and go to the ring's shared-memory tiles in the layout the operand descriptors expect; the rest
-// of those kernels does not know the difference.
+// Loader warps of the tensor-core attention kernels over a microscaled cache.  Two warps bring raw rows of 8- or 4-bit elements, and their
+// scale words, into stages of shared memory: whole tiles of consecutive rows by the copy engine, listed rows and ragged tiles by cp.async.  Four
+// others take them from there, make them bf16 and put them into the ring's tiles in the layout the operand descriptors expect; the rest of
+// those kernels does not know the difference.
 //
 // The conversion is in mx_rows.cuh.  Tiles hold the cache's values times 2^-16; the softmax scale and the division by the row sum take
 // that back.

@@ -31,9 +31,10 @@
 // All parts are added up in order.  Weights are rounded to fp16 (bf16) for the product and divided by their sum as rounded, so that they add up to
 // one; the log-sum-exp is that of the weights before.
 //
-// Measured, MXFP8 / MXFP4, us: 16 sequences of 8192 to 32768 rows, 8 KV heads of 4, d 128, one position: 132 / 128 (735 MB of MXFP8: 5.6 TB/s;
-// over a bf16 cache 557); one of 131072 rows 63 / 59, of 32768 29 / 27, of 4003 14.4.  The main kernel over 131072 rows: 867 instructions per 32 keys,
-// the issue ports busy for 48 % of the cycles, the integer pipe for 47 %.
+// Measured, MXFP8, us: 16 sequences of 8192 to 32768 rows, 8 KV heads of 4, d 128, one position: 148 among other work (735 MB: 5.0 TB/s), 134 one
+// call after the other (5.5 TB/s; over a bf16 cache 557); one of 4003 rows 14.4; 5 positions of 8 heads, d 64, MXFP4, three
+// sequences of 9001 to 20011 rows 39.4.  Before granules were looked at for their range, one call after the other, MXFP8 / MXFP4: one sequence of 131072
+// rows 63 / 59, of 32768 29 / 27; over 131072 rows 867 instructions per 32 keys, the issue ports busy for 48 % of the cycles, the integer pipe for 47 %.
 #include <algorithm>
 #include <atomic>
 
@@ -712,7 +713,8 @@ static int dec_tiles(int rows, int d) {
 
 // Query rows that these kernels take: more of them are faster in a 128-row tile of the tensor-core kernel, though it walks 128 keys for every
 // 1.0 to 1.4 us and cuts them into 8 parts at most.  These / those, us: d 128, 20 to 32 rows over 32768 keys 46 / 83, over 4003 18.4 / 22.6, over 8 sequences of
-// 8192 80 / 78; d 64, 40 rows over 3 sequences of 20011 42 / 45, 64 rows 64 / 44.
+// 8192 80 / 78; d 64, 40 rows over 3 sequences of 20011 42 / 45, 64 rows 64 / 44.  One sequence of 20011, d 64, MXFP8, 4 KV heads: 16 / 24 / 32 / 40 rows 26.7 / 28.9 /
+// 36.6 / 37.0 here (32 rows as the five tiles of 40), 48 rows in the tensor-core kernel 49.
 bool decode_mx_applies(const quoka_params* p) {
   const long long rows = (long long)p->chunk_len * (p->n_q_heads / p->n_kv_heads);
   return p->chunk_len == 1 || rows <= (p->head_dim == 64 ? 40 : 32);

@@ -66,7 +66,7 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
 // 2^(b - 127) twice, NaN for the scale byte of a block that is not finite.
 __device__ __forceinline__ uint32_t mx_scale_bf16x2(uint32_t b) { return (b == kMxNanScale ? 0x7FC0u : b == 0 ? 0x0040u : b << 7) * 0x10001u; }
 // 8 elements as bf16 values, exactly, whatever the scale: half the instructions of eight floats rounded to bf16
-// (4 sequences of 20011 to 32768 rows, 8 heads, d 128, MXFP4 read back: 101 us so, 91 this way).
+// (4 sequences of 20011 to 32768 rows, 8 heads, d 128, MXFP4 read back, one call after the other: 101 us so, 91 this way).
 template <int FMT>
 __device__ __forceinline__ uint4 mx_values_bf16x8(uint32_t w0, uint32_t w1, uint32_t scale2) {
   uint32_t o[4];

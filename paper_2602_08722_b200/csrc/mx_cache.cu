@@ -5,7 +5,8 @@
 //   the conversion instruction.  The inverse norm of a key row is that of the values the cache then holds.
 // read: cache rows first .. first + n - 1 to dense [b][n_KV][n][D] tensors; rows at and beyond T_s + C are left as they were.
 //   A lane turns 8 elements of K and of V into 16 (bf16) or 32 bytes (f32).
-// Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 91 us, 6.2 TB/s of 0.57 GB); a generation step's rows by the launch.
+// Both are bound by HBM (4 sequences of 20011 to 32768 rows, MXFP4 to bf16: 95 us among other work, 5.9 TB/s of 0.57 GB; one call after the other 90); a
+// generation step's rows by the launch.
 #include <cuda_fp16.h>
 
 #include "mx.cuh"

@@ -1,6 +1,8 @@
 // Scalar fp32 scoring and attention over the microscaled cache: what serves f32 queries, and the on-device cross-check of the
 // other kernels (QUOKA_IMPL_SIMT, both data types).  A warp per key, or per query row; the lanes split head_dim.
 // Sums as in attn_simt_kernel (compensated, online softmax).
+// Nothing is shared between the rows of a chunk, so f32 calls are far slower than over an f32 cache, which has tiled kernels.  us, MXFP8 / f32 cache,
+// 32 heads of 8, d 128, 256 queries, 1024 of 8192 rows: scoring 64 queries 321 / 40, attention 3660 / 204; one query, 512 of 8192: 24 / 10, 451 / 12.
 #include <algorithm>
 
 #include "mx.cuh"

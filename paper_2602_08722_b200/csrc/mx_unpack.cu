@@ -8,9 +8,10 @@
 // 32 columns), from where the attention kernel's epilogue makes NaN of what sees it.
 //
 // Bound by memory: 8 KV heads of 34816 rows of 128 columns, MXFP8, 73 MB in and 143 MB out; the call it belongs to, a chunk of 2048 over 32768
-// cached rows, takes 917 us against 858 us over a bf16 cache.
+// cached rows, takes 944 to 958 us among other work, where the power cap sets the pace (865 to 890 over a bf16 cache), and 825 by itself on a cool card with L2 emptied
+// (converted in the loaders 880; MXFP4 809 / 866).
 //
-// The rule (kUnpackFrom), query rows per KV head; both ways, us, converted in the loaders / unpacked first, MXFP8:
+// The rule (kUnpackFrom), query rows per KV head; both ways, us, one call after the other, converted in the loaders / unpacked first, MXFP8:
 //   listed 3932 of 32768, d 128:  1024 rows 40.2 / 42.5, 2048 57.5 / 55.4, 4096 85.7 / 79.3, 8192 170 / 147
 //   listed 3932 of 20011, d 64:   1024 rows 32.9 / 35.2, 2048 49.1 / 47.2, 3108 80.0 / 71.7
 //   all of 20011, d 64:           512 rows 57.4 / 61.6, 1024 82.0 / 81.8, 2048 148 / 137, 3108 233 / 214

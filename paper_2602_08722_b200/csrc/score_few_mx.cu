@@ -260,7 +260,8 @@ score_few_mx_kernel(DevParams P, DecWork work, const __nv_bfloat16* __restrict__
 
 // ---------------------------------------------------------------------------------------------- host
 // The tensor-core kernel takes the same for one query as for 16, 22.5 us over 32768 keys of 8 KV heads; this one 18.5 for one as for eight, the columns of a
-// matrix instruction.  16 sequences of 8192 to 32768 rows, one query, cached norms: 78 (4.9 TB/s of MXFP8; over a bf16 cache 120) / 165.
+// matrix instruction.  16 sequences of 8192 to 32768 rows, one query, cached norms: 84 among other work (4.6 TB/s of MXFP8), one call after the other 80; over a
+// bf16 cache 120; the tensor-core kernel 165.  Looking for granules that fp16 does not hold takes 2 of the 80.
 bool score_few_mx_applies(const quoka_params* p) { return std::min(p->n_retain, p->chunk_len) <= 8; }
 
 cudaError_t launch_score_few_mx(const DevParams& P, int fmt, const void* qbar, const void* k, float* scores, cudaStream_t st, bool chained) {
