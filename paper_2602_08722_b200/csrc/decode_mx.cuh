@@ -100,6 +100,8 @@ __device__ __forceinline__ float pow2_at_most_15(int diff) { return __uint_as_fl
 // (dec_scores_bf16): exact, as those of a bf16 cache, for three times the instructions.
 template <int FMT>
 constexpr int kDecKeyWindow = FMT == QUOKA_KV_MXFP8 ? 15 : 23;
+template <int FMT>
+constexpr uint32_t kMagnitudeBits = FMT == QUOKA_KV_MXFP8 ? 0x7F7F7F7Fu : 0x77777777u;     // of a word of elements
 // Columns of a query row, 8 at a time, that go with a lane's pieces of key rows.
 template <int FMT, int D>
 __device__ __forceinline__ int dec_column(int c, int j) { return FMT == QUOKA_KV_MXFP8 && D == 128 ? 16 * c + 8 * j + (j >= 2 ? 48 : 0) : c * (D / 4) + 8 * j; }
@@ -126,26 +128,26 @@ struct DecFactors {
   template <int FMT>
   __device__ __forceinline__ bool below_f16() const { return (least & 0xFFFFu) < (FMT == QUOKA_KV_MXFP8 ? 0x0200u : 0x0002u); }      // 2^-kDecKeyWindow
 };
-// Whether key row `row` of the tile at `at` (scale word sw) has such a block, not zero.
+// Whether key row `row` of the tile at `at` (scale word sw) has such a block, not zero.  (A block of zeros has the smallest scale; heads of 80 or 96
+// columns padded to 128 have one in every row: sixteen sequences of 20000 rows 130 us, 119 without, 141 by a loop over the blocks.)
 template <int FMT, int D>
 __device__ __forceinline__ bool dec_key_below_f16(uint32_t at, int row, uint32_t sw) {
+  constexpr int kBytes = 4 * kMxBits<FMT>;             // of a block: 16-byte chunks of the swizzle
   uint32_t top = __vmaxu4(sw, sw >> 16);
   top = max(top & 0xFFu, top >> 8 & 0xFFu);
-  if (top == kMxNanScale) return false;
-  bool below = false;
-#pragma unroll 1
-  for (int b = 0; b < D / kMxBlock; ++b) {
-    if ((int)(sw >> (8 * b) & 0xFFu) >= (int)top - kDecKeyWindow<FMT>) continue;
-    uint32_t any = 0;
-#pragma unroll 1
-    for (int i = 0; i < 4 * kMxBits<FMT>; i += 16) {   // 16 bytes: whole chunks of the swizzle
+  uint32_t far = top == kMxNanScale ? 0u : __vcmpltu4(sw, (uint32_t)max((int)top - kDecKeyWindow<FMT>, 0) * 0x01010101u) & (D == 128 ? 0xFFFFFFFFu : 0xFFFFu);
+  uint32_t any = 0;
+  while (far != 0u) {
+    const int b = (__ffs((int)far) - 1) / 8;
+    far &= ~(0xFFu << (8 * b));
+#pragma unroll
+    for (int i = 0; i < kBytes; i += 16) {
       uint32_t w[4];
-      lds_words<4>(at + DecBytes<FMT, D>::place(row, 4 * kMxBits<FMT> * b + i), w);
+      lds_words<4>(at + DecBytes<FMT, D>::place(row, kBytes * b + i), w);
       any |= w[0] | w[1] | w[2] | w[3];
     }
-    below |= (any & (FMT == QUOKA_KV_MXFP8 ? 0x7F7F7F7Fu : 0x77777777u)) != 0;
   }
-  return below;
+  return (any & kMagnitudeBits<FMT>) != 0;
 }
 // Products of 16 keys (rows row0 and row0 + 8 of the tile at `at` are this lane's, with scale words sw) and 8 NT query rows, bf16: sc, and of
 // the keys with themselves, where NORM.  load_q(nt, j): the lane's 8 columns of its query row.  A block that is not finite makes its key's NaN.
