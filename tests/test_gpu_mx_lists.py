@@ -70,3 +70,26 @@ def test_the_rows_in_order_give_the_same_bits_as_in_the_fused_call(fmt, n_q, n_k
         api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, out, None, P.ws)
         api.quoka_prefill_chunk_mx(P.p, P.mx, P.q, P.k, P.v, fused, None, None, P.ws)
     assert torch.equal(out, fused)
+
+
+@pytest.mark.parametrize("kind", ["twice", "any order, some twice"])
+@pytest.mark.parametrize("fmt", [api.KV_NATIVE, api.KV_MXFP8, api.KV_MXFP4])
+@pytest.mark.parametrize("n_q,n_kv,d,C", [(4, 2, 128, 1), (4, 2, 64, 70)])
+def test_a_list_as_long_as_the_cache_of_f32_queries(kind, fmt, n_q, n_kv, d, C):
+    inp = synth.make_chunk_inputs(73, 1, n_q, n_kv, d, [T], C, "f32")
+    idx = lists(n_kv, kind)
+    k_idx, k_cnt = torch.from_numpy(idx).cuda(), torch.tensor([T], dtype=torch.int32, device="cuda")
+    if fmt == api.KV_NATIVE:
+        q, k, v = inp.q.cuda(), inp.k.cuda(), inp.v.cuda()
+        out = torch.empty_like(q)
+        ctx = inp.ctx_len.cuda()
+        p = api.make_params(q, k, out, ctx, n_retain=16, kv_budget=T, max_ctx_len=T)
+        api.quoka_sparse_attn(p, q, k, v, k_idx, k_cnt, out, None, api.alloc_workspace(p))
+        k64, v64 = (x[0].double().numpy() for x in (inp.k, inp.v))
+    else:
+        P = R.MxProblem(inp, fmt, kv_budget=T, max_ctx_len=T)
+        out = P.out
+        api.quoka_sparse_attn_mx(P.p, P.mx, P.q, P.k, P.v, k_idx, k_cnt, out, None, P.ws)
+        k64, v64 = P.k64[0], P.v64[0]
+    want, _ = O.sparse_attention(inp.q[0].double().numpy(), k64[:, :T + C], v64[:, :T + C], T, [idx[0, h] for h in range(n_kv)])
+    PA.check_attention(PA.f64(out[0]), want, "f32")
